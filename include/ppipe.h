@@ -38,10 +38,16 @@ typedef enum {
     PPIPE_OP_MAXPOOL = 1,        /* k x k window, stride, padding that never wins the max */
     PPIPE_OP_AVGPOOL_GLOBAL = 2, /* mean over H x W, output 1 x 1 */
     PPIPE_OP_FC = 3,             /* y = act(W x + b) on the flattened input */
-    PPIPE_OP_FC_SOFTMAX = 4      /* p = softmax(W x + b), fp32 output; must be the range's last layer */
+    PPIPE_OP_FC_SOFTMAX = 4,     /* p = softmax(W x + b), fp32 output; must be the range's last layer */
+    PPIPE_OP_GROUPNORM = 5,      /* act of the group norm over `groups` channel groups per image */
+    PPIPE_OP_ATTENTION = 6       /* attention among the pixels of each image (a packed q|k|v map) */
 } ppipe_op;
 
-typedef enum { PPIPE_ACT_NONE = 0, PPIPE_ACT_RELU = 1, PPIPE_ACT_RELU6 = 2 } ppipe_act;
+typedef enum {
+    PPIPE_ACT_NONE = 0, PPIPE_ACT_RELU = 1, PPIPE_ACT_RELU6 = 2,
+    PPIPE_ACT_SILU = 3,          /* z / (1 + exp(-z)); GROUPNORM only */
+    PPIPE_ACT_GELU = 4           /* z (1 + erf(z / sqrt 2)) / 2; GROUPNORM only */
+} ppipe_act;
 
 typedef enum {
     PPIPE_OK = 0,
@@ -57,7 +63,18 @@ typedef enum {
  * created range.  For CONV with batch norm, all four bn_* arrays are given
  * (length c_out) and the layer computes
  *     act( (conv(x) + bias - mean) / sqrt(var + bn_eps) * gamma + beta + res ),
- * else act(conv(x) + bias + res); bias may be NULL (zero). */
+ * else act(conv(x) + bias + res); bias may be NULL (zero).
+ *
+ * GROUPNORM (c_in = c_out, no residual) computes
+ *     act( (x - mean) / sqrt(var + bn_eps) * gamma + beta )
+ * with the mean and the biased variance of each image's `groups` groups of
+ * consecutive channels over all its pixels; bn_gamma, bn_beta [c_out] or NULL
+ * (1 and 0), bn_eps > 0 or the default 1e-5, any ppipe_act; bn_mean and bn_var are not read.
+ *
+ * ATTENTION reads a map whose channels are q | k | v, (heads + 2 kv_heads) x
+ * head_dim in all, and writes heads x head_dim channels; what else it needs is
+ * its ppipe_attention_layer (ppipe_partition_create_attention).  No residual,
+ * no activation. */
 typedef struct {
     int32_t op;          /* ppipe_op */
     int32_t src;         /* producer layer index, -1 = model input */
@@ -67,7 +84,7 @@ typedef struct {
     int32_t k;           /* square window (CONV, MAXPOOL) */
     int32_t stride;
     int32_t pad;
-    int32_t groups;      /* 1, or c_in (== c_out) for depthwise */
+    int32_t groups;      /* 1, or c_in (== c_out) for depthwise; GROUPNORM: its groups */
     int32_t act;         /* ppipe_act */
     const float* weight; /* CONV [c_out][c_in/groups][k][k]; FC [c_out][c_in] */
     const float* bias;   /* [c_out] or NULL */
@@ -189,6 +206,34 @@ ppipe_partition* ppipe_partition_create_on_share(const ppipe_model_desc* desc,
                                                  int32_t layer_begin, int32_t layer_end,
                                                  int32_t dtype, int32_t parts);
 
+/* What an ATTENTION layer computes beyond its channels.  Pixels are tokens in
+ * row-major order; positions are (row, column).  As ppipe_attention, and
+ * ppipe_rotary on the query and key heads first. */
+typedef struct {
+    int32_t layer;             /* index of the ATTENTION layer */
+    int32_t heads, kv_heads;   /* heads a multiple of kv_heads; head_dim = c_out / heads */
+    float scale;               /* of the scores; 0: 1 / sqrt(head_dim) */
+    float softcap;             /* 0: none */
+    const float* slopes;       /* host [heads]: distance bias, or NULL; read during create */
+    int32_t causal;            /* nonzero: a pixel sees itself and the pixels before it ... */
+    int32_t prefix;            /* ... and the first `prefix` pixels (0: none) */
+    int32_t rotary_pairs[2];   /* rotated pairs by row and by column; both 0: no rotary */
+    int32_t rotary_shared;     /* as in ppipe_rotary_desc */
+    int32_t rotary_adjacent;
+    double rotary_base;        /* 0: 10000 */
+} ppipe_attention_layer;
+
+/* ppipe_partition_create for ranges with ATTENTION layers: attention holds one
+ * ppipe_attention_layer for each of them in the range (entries of layers outside
+ * the range are ignored; a missing, doubled or misplaced one is PPIPE_E_INVALID).  parts as in
+ * ppipe_partition_create_on_share (1: the whole device).  The other create
+ * calls refuse a range with an ATTENTION layer. */
+ppipe_partition* ppipe_partition_create_attention(const ppipe_model_desc* desc,
+                                                  int32_t layer_begin, int32_t layer_end,
+                                                  int32_t dtype,
+                                                  const ppipe_attention_layer* attention,
+                                                  int32_t n_attention, int32_t parts);
+
 /* Forward pass of the range at batch size `batch` (1..max_batch).
  * in:  device pointer, [batch][in_h][in_w][in_c] in dtype (caller-owned).
  * out: device pointer, [batch][out_h][out_w][out_c] in out_dtype (caller-owned);
@@ -268,6 +313,111 @@ int ppipe_profile_kernels(ppipe_partition* h, int32_t batch, int32_t warmup,
  * null buffer with n > 0). */
 int ppipe_cast(const void* in, int32_t in_dtype, void* out, int32_t out_dtype, int64_t n,
                void* stream);
+
+/* ---- operators on device tensors ----
+ *
+ * One call each on the current HIP device, asynchronous on `stream` (a
+ * hipStream_t, NULL = default stream): no allocation, no host synchronisation,
+ * so a caller may capture them into its own HIP graph.  Scratch memory is the
+ * caller's: calls whose work may overlap in time need workspaces of their own,
+ * and so do graphs that may replay side by side.  Contents of a workspace are
+ * not kept from call to call.  Sums, statistics and softmax are fp32; outputs
+ * are rounded to dtype once, to nearest even.  Results do not vary from run to
+ * run.  Sizes of zero launch nothing and succeed.  Device pointers and strides
+ * are 16-byte aligned unless stated; strides count elements. */
+
+/* Group norm with an activation over densely packed NHWC maps: x, y [batch]
+ * [pixels][channels] in dtype,
+ *     y = act( (x - mean) / sqrt(var + eps) * gamma + beta ),
+ * mean and biased variance over each image's pixels x (channels / groups)
+ * consecutive channels.  gamma, beta: device fp32 [channels] (4-byte aligned),
+ * or NULL for 1 and 0.  y may be x; other overlaps are not allowed.
+ * channels: a multiple of groups and of one 16-byte vector, at most 65536 (PPIPE_E_UNSUPPORTED
+ * otherwise); eps >= 0 and finite.  workspace: ppipe_group_norm_workspace bytes (may be
+ * NULL when that is 0).  A NaN or infinity makes its group's outputs NaN.
+ * Returns a status. */
+int64_t ppipe_group_norm_workspace(int32_t dtype, int32_t batch, int32_t pixels,
+                                   int32_t channels, int32_t groups);
+int ppipe_group_norm(const void* x, void* y, int32_t dtype, int32_t batch, int32_t pixels,
+                     int32_t channels, int32_t groups, const float* gamma, const float* beta,
+                     float eps, int32_t act, void* workspace, int64_t workspace_bytes,
+                     void* stream);
+
+/* Rotary positions with one to three axes (time, height, width of a clip).
+ * Rotated pairs p = 0 .. P-1, P = pairs[0] + ... of the axes in order; pair p is
+ * the i-th of its axis a's n = pairs[a] and turns by the angle
+ *     positions[a] * base^(-i / n)    (shared = 0: a ladder of its own per axis)
+ *     positions[a] * base^(-p / P)    (shared = 1: one ladder over all pairs)
+ * (u, w) -> (u cos - w sin, u sin + w cos), where the pair's elements are p and
+ * p + P of a head (adjacent = 0) or 2p and 2p + 1 (adjacent = 1).  Elements from
+ * 2 P on are copied.  Angles are reduced in 64 bits, so far positions keep
+ * their precision. */
+typedef struct {
+    int32_t dtype;
+    int32_t batch, tokens, heads, head_dim;   /* head_dim: a multiple of 8, at most 256 */
+    int32_t axes;                             /* 1 .. 3 */
+    int32_t pairs[3];                         /* >= 0, one to head_dim / 2 in all */
+    int32_t shared, adjacent;                 /* 0 or 1 */
+    double base;                              /* > 0 */
+    int64_t x_strides[3], y_strides[3];       /* between batch items, tokens, heads */
+    int64_t positions_stride;                 /* between batch items; 0: the same for all */
+} ppipe_rotary_desc;
+
+/* positions: device int32 [batch][tokens][axes] (4-byte aligned, any values).
+ * Query and key heads that lie side by side in a packed map take one call.  y
+ * may be x with the same strides; other overlaps are not allowed, and y's own
+ * elements must not overlap (PPIPE_E_INVALID).  Returns a status. */
+int ppipe_rotary(const ppipe_rotary_desc* desc, const void* x, const int32_t* positions, void* y,
+                 void* stream);
+
+/* The keys that each query may see, for any number of ppipe_attention calls
+ * with the same mask: spans [batch][q_len][2] receives first and end.  Query i
+ * of batch item b is at position q_start[b] + i (NULL: i) among the keys and
+ * sees its document: the d with doc_offsets[b][d] <= position <
+ * doc_offsets[b][d + 1] (NULL: n_docs is 1, the document is [0, kv_len)).
+ * causal: of it, the keys up to its own position and the document's first
+ * prefix[b][d] keys (NULL: none; not read otherwise).  A query in no document sees nothing (0, 0).
+ * doc_offsets: device int32 [batch][n_docs + 1], not decreasing; values outside
+ * [0, kv_len] are taken as the nearer end.  All pointers device memory, 4-byte
+ * aligned (spans 8).  Returns a status. */
+int ppipe_attention_spans(int32_t* spans, int32_t batch, int32_t q_len, int32_t kv_len,
+                          const int32_t* doc_offsets, int32_t n_docs, const int32_t* prefix,
+                          int32_t causal, const int32_t* q_start, void* stream);
+
+/* Attention:  out_i = sum_j softmax_j(s_ij) v_j over the keys j that query i sees,
+ *     s = scale q_i . k_j;
+ *     s = softcap tanh(s / softcap)                       (softcap > 0)
+ *     s = s - slopes[head] sum_a |q_position_ia - k_position_ja|   (slopes given)
+ * Query head h reads key head h / (heads / kv_heads).  A query that sees no key
+ * gets zeros, and so does one whose scores are all -inf.  Keys that a query does not see never change its
+ * output, whatever they hold (NaN and infinities included). */
+typedef struct {
+    int32_t dtype;
+    int32_t batch, q_len, kv_len;
+    int32_t heads, kv_heads, head_dim;        /* head_dim: a multiple of 8, at most 256 */
+    float scale, softcap;                     /* finite; softcap 0: none */
+    int32_t axes;                             /* of the positions, 1 .. 3; 0 without slopes */
+    int64_t q_strides[3], k_strides[3], v_strides[3], out_strides[3];
+                                              /* between batch items, tokens, heads; below 2^22
+                                                 between tokens and heads */
+    int64_t q_positions_stride, k_positions_stride;   /* between batch items; 0: shared */
+    int64_t spans_stride;                     /* between batch items; 0: shared */
+} ppipe_attention_desc;
+
+/* Scratch bytes of a call (0: none), or a negative status. */
+int64_t ppipe_attention_workspace(const ppipe_attention_desc* desc);
+
+/* q, out: [batch][q_len][heads][head_dim], k, v: [batch][kv_len][kv_heads]
+ * [head_dim] in dtype, by their strides (batch items of k and v may share
+ * memory).  slopes: device fp32 [heads] with q_positions, k_positions: device
+ * int32 [batch][q_len or kv_len][axes], or all three NULL.  spans: device int32
+ * [batch][q_len][2], first and end of the keys that a query sees (cut to
+ * [0, kv_len]); NULL: all.  out must not overlap the inputs or itself.
+ * workspace: ppipe_attention_workspace bytes.  Returns a status. */
+int ppipe_attention(const ppipe_attention_desc* desc, const void* q, const void* k, const void* v,
+                    void* out, const float* slopes, const int32_t* q_positions,
+                    const int32_t* k_positions, const int32_t* spans, void* workspace,
+                    int64_t workspace_bytes, void* stream);
 
 /* Virtual GPUs (Sec. 5.3: a physical GPU split into 1/1, 1/2, 1/3 or 1/4
  * shares; the paper uses MPS).  Creates a stream, at default priority, on

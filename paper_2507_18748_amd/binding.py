@@ -13,8 +13,9 @@ import numpy as np
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libppipe.so")
 
-OPS = {"conv": 0, "maxpool": 1, "gap": 2, "fc": 3, "fc_softmax": 4}
-ACTS = {"none": 0, "relu": 1, "relu6": 2}
+OPS = {"conv": 0, "maxpool": 1, "gap": 2, "fc": 3, "fc_softmax": 4, "groupnorm": 5,
+       "attention": 6}
+ACTS = {"none": 0, "relu": 1, "relu6": 2, "silu": 3, "gelu": 4}
 DTYPES = {"f32": 0, "f16": 1, "bf16": 2}
 
 _fp = ctypes.POINTER(ctypes.c_float)
@@ -42,6 +43,37 @@ class ModelDesc(ctypes.Structure):
     _fields_ = [("n_layers", ctypes.c_int32), ("layers", ctypes.POINTER(LayerDesc)),
                 ("in_c", ctypes.c_int32), ("in_h", ctypes.c_int32), ("in_w", ctypes.c_int32),
                 ("max_batch", ctypes.c_int32)]
+
+
+class AttentionLayer(ctypes.Structure):
+    """What an attention layer of a partition computes (ppipe_attention_layer)."""
+    _fields_ = [("layer", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("softcap", ctypes.c_float), ("slopes", _fp), ("causal", ctypes.c_int32),
+                ("prefix", ctypes.c_int32), ("rotary_pairs", ctypes.c_int32 * 2),
+                ("rotary_shared", ctypes.c_int32), ("rotary_adjacent", ctypes.c_int32),
+                ("rotary_base", ctypes.c_double)]
+
+
+_i64x3 = ctypes.c_int64 * 3
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("tokens", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("pairs", ctypes.c_int32 * 3), ("shared", ctypes.c_int32),
+                ("adjacent", ctypes.c_int32), ("base", ctypes.c_double), ("x_strides", _i64x3),
+                ("y_strides", _i64x3), ("positions_stride", ctypes.c_int64)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_len", ctypes.c_int32),
+                ("kv_len", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("axes", ctypes.c_int32),
+                ("q_strides", _i64x3), ("k_strides", _i64x3), ("v_strides", _i64x3),
+                ("out_strides", _i64x3), ("q_positions_stride", ctypes.c_int64),
+                ("k_positions_stride", ctypes.c_int64), ("spans_stride", ctypes.c_int64)]
 
 
 def _records(recs, count: int, cap: int) -> List[dict]:
@@ -143,6 +175,9 @@ def load_library() -> ctypes.CDLL:
                                                  ctypes.POINTER(Tuning)]
     lib.ppipe_partition_create_on_share.restype = vp
     lib.ppipe_partition_create_on_share.argtypes = [ctypes.POINTER(ModelDesc), i32, i32, i32, i32]
+    lib.ppipe_partition_create_attention.restype = vp
+    lib.ppipe_partition_create_attention.argtypes = [ctypes.POINTER(ModelDesc), i32, i32, i32,
+                                                     ctypes.POINTER(AttentionLayer), i32, i32]
     lib.ppipe_partition_run.restype = ctypes.c_int
     lib.ppipe_partition_run.argtypes = [vp, i32, vp, vp, vp]
     lib.ppipe_partition_run_static_scratch.restype = ctypes.c_int
@@ -177,6 +212,21 @@ def load_library() -> ctypes.CDLL:
     lib.ppipe_stream_destroy.argtypes = [vp]
     lib.ppipe_cast.restype = ctypes.c_int
     lib.ppipe_cast.argtypes = [vp, i32, vp, i32, ctypes.c_int64, vp]
+    i64, f32 = ctypes.c_int64, ctypes.c_float
+    lib.ppipe_group_norm_workspace.restype = i64
+    lib.ppipe_group_norm_workspace.argtypes = [i32] * 5
+    lib.ppipe_group_norm.restype = ctypes.c_int
+    lib.ppipe_group_norm.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, f32, i32, vp, i64,
+                                     vp]
+    lib.ppipe_rotary.restype = ctypes.c_int
+    lib.ppipe_rotary.argtypes = [ctypes.POINTER(RotaryDesc), vp, vp, vp, vp]
+    lib.ppipe_attention_spans.restype = ctypes.c_int
+    lib.ppipe_attention_spans.argtypes = [vp, i32, i32, i32, vp, i32, vp, i32, vp, vp]
+    lib.ppipe_attention_workspace.restype = i64
+    lib.ppipe_attention_workspace.argtypes = [ctypes.POINTER(AttentionDesc)]
+    lib.ppipe_attention.restype = ctypes.c_int
+    lib.ppipe_attention.argtypes = [ctypes.POINTER(AttentionDesc), vp, vp, vp, vp, vp, vp, vp,
+                                    vp, vp, i64, vp]
     lib.ppipe_split_points.restype = ctypes.c_int
     lib.ppipe_split_points.argtypes = [ctypes.POINTER(ModelDesc), ctypes.POINTER(i32)]
     lib.ppipe_prepartition.restype = ctypes.c_int
@@ -235,6 +285,103 @@ def cast(x_ptr: int, in_dtype: str, y_ptr: int, out_dtype: str, n: int, stream: 
     """Boundary quantisation: n elements converted on the device (ppipe_cast)."""
     lib = load_library()
     status = lib.ppipe_cast(x_ptr, DTYPES[in_dtype], y_ptr, DTYPES[out_dtype], n, stream)
+    if status != 0:
+        raise _err(lib, status)
+
+
+def group_norm_workspace(dtype: str, batch: int, pixels: int, channels: int, groups: int) -> int:
+    """Scratch bytes of a group_norm call (ppipe_group_norm_workspace)."""
+    lib = load_library()
+    n = lib.ppipe_group_norm_workspace(DTYPES[dtype], batch, pixels, channels, groups)
+    if n < 0:
+        raise _err(lib, n)
+    return n
+
+
+def group_norm(x_ptr: int, y_ptr: int, dtype: str, batch: int, pixels: int, channels: int,
+               groups: int, gamma_ptr: int = 0, beta_ptr: int = 0, eps: float = 1e-5,
+               act: str = "none", workspace_ptr: int = 0, workspace_bytes: int = 0,
+               stream: int = 0):
+    """Group norm with an activation over [batch][pixels][channels] (ppipe_group_norm).
+    Device addresses; gamma and beta are fp32 [channels], 0 for 1 and 0."""
+    lib = load_library()
+    status = lib.ppipe_group_norm(x_ptr, y_ptr, DTYPES[dtype], batch, pixels, channels, groups,
+                                  gamma_ptr, beta_ptr, eps, ACTS[act], workspace_ptr,
+                                  workspace_bytes, stream)
+    if status != 0:
+        raise _err(lib, status)
+
+
+def rotary(x_ptr: int, y_ptr: int, dtype: str, batch: int, tokens: int, heads: int,
+           head_dim: int, pairs: Sequence[int], positions_ptr: int, positions_stride: int,
+           x_strides: Sequence[int], y_strides: Sequence[int], base: float = 10000.0,
+           shared: bool = False, adjacent: bool = False, stream: int = 0):
+    """Rotary positions with len(pairs) axes on [batch][tokens][heads][head_dim]
+    (ppipe_rotary).  pairs: rotated pairs of each axis; positions: int32
+    [batch][tokens][axes] with positions_stride elements between batch items (0:
+    the same for all); strides between batch items, tokens and heads, in elements."""
+    lib = load_library()
+    axes = len(pairs)
+    if axes > 3:
+        raise PpipeError(-1, "rotary takes one to three axes")
+    desc = RotaryDesc(DTYPES[dtype], batch, tokens, heads, head_dim, axes,
+                      (ctypes.c_int32 * 3)(*pairs), bool(shared), bool(adjacent), base,
+                      _i64x3(*x_strides), _i64x3(*y_strides), positions_stride)
+    status = lib.ppipe_rotary(ctypes.byref(desc), x_ptr, positions_ptr, y_ptr, stream)
+    if status != 0:
+        raise _err(lib, status)
+
+
+def attention_spans(spans_ptr: int, batch: int, q_len: int, kv_len: int,
+                    doc_offsets_ptr: int = 0, n_docs: int = 1, prefix_ptr: int = 0,
+                    causal: bool = False, q_start_ptr: int = 0, stream: int = 0):
+    """First and end of the keys that each query sees, int32 [batch][q_len][2]
+    (ppipe_attention_spans): documents, causal, prefixes, filled lengths."""
+    lib = load_library()
+    status = lib.ppipe_attention_spans(spans_ptr, batch, q_len, kv_len, doc_offsets_ptr, n_docs,
+                                       prefix_ptr, int(causal), q_start_ptr, stream)
+    if status != 0:
+        raise _err(lib, status)
+
+
+def attention_desc(dtype: str, batch: int, q_len: int, kv_len: int, heads: int, kv_heads: int,
+                   head_dim: int, q_strides: Sequence[int], k_strides: Sequence[int],
+                   v_strides: Sequence[int], out_strides: Sequence[int], scale: float,
+                   softcap: float = 0.0, axes: int = 0, q_positions_stride: int = 0,
+                   k_positions_stride: int = 0, spans_stride: int = 0) -> AttentionDesc:
+    """ppipe_attention_desc; strides between batch items, tokens and heads, in elements."""
+    return AttentionDesc(DTYPES[dtype], batch, q_len, kv_len, heads, kv_heads, head_dim, scale,
+                         softcap, axes, _i64x3(*q_strides), _i64x3(*k_strides),
+                         _i64x3(*v_strides), _i64x3(*out_strides), q_positions_stride,
+                         k_positions_stride, spans_stride)
+
+
+def attention_workspace(desc: AttentionDesc) -> int:
+    """Scratch bytes of an attention call (ppipe_attention_workspace)."""
+    lib = load_library()
+    n = lib.ppipe_attention_workspace(ctypes.byref(desc))
+    if n < 0:
+        raise _err(lib, n)
+    return n
+
+
+def attention(q_ptr: int, k_ptr: int, v_ptr: int, out_ptr: int, dtype: str, batch: int,
+              q_len: int, kv_len: int, heads: int, kv_heads: int, head_dim: int,
+              q_strides: Sequence[int], k_strides: Sequence[int], v_strides: Sequence[int],
+              out_strides: Sequence[int], scale: float, softcap: float = 0.0,
+              slopes_ptr: int = 0, q_positions_ptr: int = 0, k_positions_ptr: int = 0,
+              axes: int = 0, q_positions_stride: int = 0, k_positions_stride: int = 0,
+              spans_ptr: int = 0, spans_stride: int = 0, workspace_ptr: int = 0,
+              workspace_bytes: int = 0, stream: int = 0):
+    """Attention over strided [batch][token][head][head_dim] tensors (ppipe_attention):
+    optional score cap, distance bias (slopes and positions) and spans of visible keys."""
+    lib = load_library()
+    desc = attention_desc(dtype, batch, q_len, kv_len, heads, kv_heads, head_dim, q_strides,
+                          k_strides, v_strides, out_strides, scale, softcap, axes,
+                          q_positions_stride, k_positions_stride, spans_stride)
+    status = lib.ppipe_attention(ctypes.byref(desc), q_ptr, k_ptr, v_ptr, out_ptr, slopes_ptr,
+                                 q_positions_ptr, k_positions_ptr, spans_ptr, workspace_ptr,
+                                 workspace_bytes, stream)
     if status != 0:
         raise _err(lib, status)
 
@@ -384,6 +531,9 @@ class Partition:
       c_out, k, stride, pad, groups, act (op / act as names, see OPS / ACTS).
     params: {layer index: {"weight", "bias", "bn_gamma", "bn_beta", "bn_mean",
       "bn_var"}} of float32 numpy arrays (OIHW weights); read during create.
+    attention: {layer index: dict of AttentionLayer fields (heads, kv_heads, scale, softcap,
+      slopes, causal, prefix, rotary_pairs, rotary_shared, rotary_adjacent,
+      rotary_base)} for the range's attention layers.  Not combined with tuning.
     tuning: planner overrides for kernel tests and tuning sweeps, a dict of
       Tuning fields (gemm_plan=(cfg, waves, splits) sets the first three);
       None (the default) leaves every choice to the planner.
@@ -395,7 +545,8 @@ class Partition:
     def __init__(self, layers: Sequence, params: Dict[int, Dict[str, np.ndarray]],
                  in_chw: Sequence[int], begin: int, end: int, dtype: str,
                  max_batch: int = 64, bn_eps: float = 1e-5, tuning: Optional[dict] = None,
-                 cu_share_parts: Optional[int] = None):
+                 cu_share_parts: Optional[int] = None,
+                 attention: Optional[Dict[int, dict]] = None):
         self._lib = load_library()
         self.begin, self.end, self.dtype = begin, end, dtype
         keep: List[np.ndarray] = []
@@ -434,7 +585,27 @@ class Partition:
                          int(max_batch))
         if tuning and cu_share_parts not in (None, 1):
             raise ValueError("tuning overrides plan for the whole device; drop cu_share_parts")
-        if tuning:
+        if tuning and attention:
+            raise ValueError("tuning overrides and attention layers do not combine")
+        if attention:
+            att = (AttentionLayer * len(attention))()
+            for d, (i, a) in zip(att, attention.items()):
+                d.layer, d.kv_heads = i, a.get("kv_heads", a["heads"])
+                for k, v in a.items():
+                    if k == "slopes":
+                        if v is not None and len(v) != a["heads"]:
+                            raise ValueError("one slope for each head")
+                        d.slopes = ptr(v)
+                    elif k == "rotary_pairs":
+                        d.rotary_pairs = (ctypes.c_int32 * 2)(*v)
+                    elif k in dict(AttentionLayer._fields_) and k != "layer":
+                        setattr(d, k, v)
+                    else:
+                        raise ValueError(f"unknown attention field {k!r}")
+            h = self._lib.ppipe_partition_create_attention(
+                ctypes.byref(desc), begin, end, DTYPES[dtype], att, len(attention),
+                1 if cu_share_parts is None else int(cu_share_parts))
+        elif tuning:
             t = Tuning(-1, 0, 1, 0, 0, 0, 0, 0)
             for k, v in tuning.items():
                 if k == "gemm_plan":

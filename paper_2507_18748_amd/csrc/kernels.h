@@ -29,7 +29,7 @@ LaunchEvents& launch_events();
         else                                                                                     \
             hipLaunchKernelGGL(KERNEL, GRID, BLOCK, SHMEM, STREAM, __VA_ARGS__);                 \
     } while (0)
-enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_RELU6 = 2 };
+enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_RELU6 = 2, ACT_SILU = 3, ACT_GELU = 4 };
 
 // Records a failing call's status and message for ppipe_last_error(); returns status.
 int set_error(int status, const std::string& msg);
@@ -296,6 +296,63 @@ const char* maxpool_name(int dt);
 // Mean over H x W per (n, c), fp32 sum, NHWC in -> [N][C] out.
 hipError_t launch_gap(int dt, const void* x, void* y, int N, int HW, int C, hipStream_t s);
 const char* gap_name(int dt);
+
+// Group norm with an activation, NHWC [N][P][C]; gamma, beta [C] or null.
+// C % (16 / sizeof(dtype)) == 0.  ws: group_norm_workspace bytes.
+struct GroupNormArgs {
+    const void* x;
+    void* y;
+    const float *gamma, *beta;
+    int N, P, C, G;
+    float eps;
+    int act;
+};
+size_t group_norm_workspace(int dt, int N, int P, int C, int G, int cus);
+// one of the group_norm_launches
+hipError_t launch_group_norm(int dt, const GroupNormArgs& a, void* ws, int cus, int launch,
+                             hipStream_t s);
+const char* group_norm_name(int dt, int N, int P, int C, int G, int cus, int launch);
+int group_norm_launches(int dt, int N, int P, int C, int G, int cus);
+
+// Rotary positions: x, y [N][L][H][d] by strides (batch, token, head).
+struct RotaryArgs {
+    const void* x;
+    void* y;
+    const int* pos;       // [N][L][A]
+    int N, L, H, d, A;
+    int pairs[3];
+    int shared, adjacent;
+    double base;
+    int64_t xs[3], ys[3], ps;
+};
+hipError_t launch_rotary(int dt, const RotaryArgs& a, hipStream_t s);
+const char* rotary_name(int dt);
+
+// Spans of visible keys (ppipe_attention_spans).
+struct SpansArgs {
+    int* spans;
+    const int *offsets, *prefix, *start;
+    int N, Lq, Lk, docs, causal;
+};
+hipError_t launch_attention_spans(const SpansArgs& a, hipStream_t s);
+
+// Attention over [N][L][H][d] tensors by strides (batch, token, head).
+struct AttentionArgs {
+    const void *q, *k, *v;
+    void* out;
+    const float* slopes;            // [H] or null
+    const int *qpos, *kpos;         // [N][L][A]
+    const int* spans;               // [N][Lq][2] or null
+    int N, Lq, Lk, H, Hk, d, A;
+    float scale, cap;
+    int64_t qs[3], ks[3], vs[3], os[3], qps, kps, sps;
+};
+size_t attention_workspace(int dt, const AttentionArgs& a, int cus);
+// one of the attention_launches
+hipError_t launch_attention(int dt, const AttentionArgs& a, void* ws, int cus, int launch,
+                            hipStream_t s);
+int attention_launches(int dt, const AttentionArgs& a, int cus);
+const char* attention_name(int dt, const AttentionArgs& a, int cus, int launch);
 
 // n elements of x (in_dt) converted to y (out_dt); narrowing rounds to
 // nearest even.

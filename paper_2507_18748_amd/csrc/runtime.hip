@@ -14,6 +14,7 @@
 //   Sec. 5.1 offline profiling).
 #include "ppipe.h"
 #include "kernels.h"
+#include "operators.h"
 
 #include <algorithm>
 #include <cmath>
@@ -92,7 +93,7 @@ void put_elem(std::vector<uint8_t>& blob, size_t off, int dt, size_t i, float v)
     }
 }
 
-enum Kind { K_GEMM = 0, K_DW = 1, K_MAXPOOL = 2, K_GAP = 3 };
+enum Kind { K_GEMM = 0, K_DW = 1, K_MAXPOOL = 2, K_GAP = 3, K_NORM = 4, K_ATTN = 5 };
 enum { BUF_IN = -1, BUF_OUT = -2, BUF_NONE = -3 };
 
 struct Plan {
@@ -112,7 +113,9 @@ struct FusePlan {
 };
 
 // Scratch memory of a run: split-K partial sums followed by the fp32 logits
-// of a final FC + softmax (ws), and the channel-padded input of a stem (pad).
+// of a final FC + softmax, the statistics of a group norm, or the rotated heads
+// and partial results of an attention layer (ws), and the channel-padded input
+// of a stem (pad).
 struct Workspace {
     float* ws;
     void* pad;
@@ -150,6 +153,13 @@ struct LayerRT {
     int fuse_pos = -1;
     std::vector<FusePlan> fuse_plans;
     std::vector<Plan> plans;   // [batch - 1]
+    // attention: its description, and offsets of the slopes, the pixels'
+    // positions and their spans of visible keys among the parameters
+    ppipe_attention_layer att{};
+    float eps = 0.0f;          // group norm
+    size_t pos_off = 0, spans_off = 0;
+    const int* pos = nullptr;
+    const int* spans = nullptr;
     std::string name;          // the description's layer name, or "layer<i>"
     int64_t out_bytes_b1 = 0;
     double flops_b1 = 0, in_bytes_b1 = 0, res_bytes_b1 = 0, param_bytes = 0;
@@ -173,7 +183,7 @@ struct ppipe_partition {
     std::vector<LayerRT> L;
     std::vector<void*> slots;
     std::vector<size_t> slot_bytes;
-    float* ws = nullptr;          // split-K partials, then fp32 logits of a final FC + softmax
+    float* ws = nullptr;          // scratch of a layer's launches (Workspace)
     size_t ws_bytes = 0;
     void* pad_buf = nullptr;      // channel-padded input of layers with C < 16 bytes
     size_t pad_bytes = 0;
@@ -496,11 +506,87 @@ struct TimedHook : LaunchHook {
     }
 };
 
-// Launch sequence of a GEMM layer: [channel pad], GEMM, [split-K reduce], [softmax].
-enum LaunchRole { L_PAD, L_GEMM, L_REDUCE, L_SOFTMAX, L_OTHER };
-
-std::vector<int> launch_roles(const LayerRT& l, int batch)
+// ---- group norm and attention layers ----
+GroupNormArgs norm_args(const LayerRT& l, int batch, const void* x, void* y)
 {
+    return GroupNormArgs{x, y, l.scale, l.bias, batch, l.H * l.W, l.C, l.groups, l.eps, l.act};
+}
+
+bool rotates(const LayerRT& l) { return l.att.rotary_pairs[0] + l.att.rotary_pairs[1] > 0; }
+
+// The rotary pass of an attention layer: query and key heads of the packed map
+// into [batch][pixel][heads + kv_heads][head_dim].
+ppipe_rotary_desc rotary_desc(const LayerRT& l, int dt, int batch)
+{
+    const int d = l.Co / l.att.heads, heads = l.att.heads + l.att.kv_heads;
+    const int64_t hw = (int64_t)l.H * l.W;
+    return ppipe_rotary_desc{dt, batch, (int32_t)hw, heads, d, 2,
+                             {l.att.rotary_pairs[0], l.att.rotary_pairs[1], 0},
+                             l.att.rotary_shared, l.att.rotary_adjacent, l.att.rotary_base,
+                             {hw * l.C, l.C, d}, {hw * heads * d, (int64_t)heads * d, d}, 0};
+}
+
+ppipe_attention_desc attention_desc(const LayerRT& l, int dt, int batch)
+{
+    const int d = l.Co / l.att.heads, heads = l.att.heads + l.att.kv_heads;
+    const int64_t hw = (int64_t)l.H * l.W, row = rotates(l) ? (int64_t)heads * d : l.C;
+    return ppipe_attention_desc{dt, batch, (int32_t)hw, (int32_t)hw, l.att.heads, l.att.kv_heads,
+                                d, l.att.scale, l.att.softcap, l.att.slopes ? 2 : 0,
+                                {hw * row, row, d}, {hw * row, row, d}, {hw * l.C, l.C, d},
+                                {hw * l.Co, l.Co, d}, 0, 0, 0};
+}
+
+size_t rotated_bytes(const LayerRT& l, int dt, int batch)
+{
+    if (!rotates(l)) return 0;
+    const size_t n = (size_t)batch * l.H * l.W * (l.att.heads + l.att.kv_heads) *
+                     (l.Co / l.att.heads) * dtype_size(dt);
+    return (n + 255) / 256 * 256;
+}
+
+AttentionArgs layer_attention(const LayerRT& l, int dt, int batch, const void* x, void* y,
+                              const void* rotated)
+{
+    const size_t head = (size_t)(l.Co / l.att.heads) * dtype_size(dt);
+    const uint8_t* q = (const uint8_t*)(rotates(l) ? rotated : x);
+    return attention_args(attention_desc(l, dt, batch), q, q + head * l.att.heads,
+                          (const uint8_t*)x + head * (l.att.heads + l.att.kv_heads), y,
+                          l.att.slopes ? l.scale : nullptr, l.att.slopes ? l.pos : nullptr,
+                          l.att.slopes ? l.pos : nullptr, l.spans);
+}
+
+// Scratch bytes of a group norm or attention layer.
+size_t layer_scratch(const ppipe_partition* P, const LayerRT& l, int batch)
+{
+    if (l.kind == K_NORM)
+        return group_norm_workspace(P->dtype, batch, l.H * l.W, l.C, l.groups, P->cus);
+    if (l.kind == K_ATTN)
+        return rotated_bytes(l, P->dtype, batch) +
+               attention_workspace(P->dtype, layer_attention(l, P->dtype, batch, nullptr, nullptr,
+                                                             nullptr), P->cus);
+    return 0;
+}
+
+// Launch sequence of a GEMM layer: [channel pad], GEMM, [split-K reduce],
+// [softmax]; of a group norm: [statistics], outputs; of an attention layer:
+// [rotary], attention, [join].
+enum LaunchRole { L_PAD, L_GEMM, L_REDUCE, L_SOFTMAX, L_OTHER, L_STATS, L_NORM, L_ROTARY, L_ATTN,
+                  L_JOIN };
+
+std::vector<int> launch_roles(const ppipe_partition* P, const LayerRT& l, int batch)
+{
+    if (l.kind == K_NORM)
+        return group_norm_launches(P->dtype, batch, l.H * l.W, l.C, l.groups, P->cus) > 1
+                   ? std::vector<int>{L_STATS, L_NORM} : std::vector<int>{L_NORM};
+    if (l.kind == K_ATTN) {
+        std::vector<int> r;
+        if (rotates(l)) r.push_back(L_ROTARY);
+        r.push_back(L_ATTN);
+        if (attention_launches(P->dtype, layer_attention(l, P->dtype, batch, nullptr, nullptr,
+                                                         nullptr), P->cus) > 1)
+            r.push_back(L_JOIN);
+        return r;
+    }
     if (l.kind != K_GEMM) return {L_OTHER};
     std::vector<int> r;
     if (pads_input(l, l.plans[batch - 1])) r.push_back(L_PAD);
@@ -538,7 +624,7 @@ bool fuse_runs(const ppipe_partition* P, const LayerRT& l, int batch, bool apart
 int layer_launches(const ppipe_partition* P, const LayerRT& l, int batch, bool apart = false)
 {
     if (fuse_runs(P, l, batch, apart)) return l.fuse_pos == 0 ? 1 : 0;
-    return (int)launch_roles(l, batch).size();
+    return (int)launch_roles(P, l, batch).size();
 }
 
 std::string launch_name(const ppipe_partition* P, const LayerRT& l, int batch, int launch)
@@ -546,7 +632,7 @@ std::string launch_name(const ppipe_partition* P, const LayerRT& l, int batch, i
     switch (l.kind) {
     case K_GEMM: {
         const Plan& p = l.plans[batch - 1];
-        switch (launch_roles(l, batch)[launch]) {
+        switch (launch_roles(P, l, batch)[launch]) {
         case L_PAD: return pad_channels_name(P->dtype);
         case L_GEMM: return conv_gemm_name(P->dtype, p.cfg, p.wk, tapv_of(l, p));
         case L_REDUCE: return splitk_reduce_name(P->dtype);
@@ -555,6 +641,12 @@ std::string launch_name(const ppipe_partition* P, const LayerRT& l, int batch, i
     }
     case K_DW: return dwconv_name(P->dtype, l.k);
     case K_MAXPOOL: return maxpool_name(P->dtype);
+    case K_NORM: return group_norm_name(P->dtype, batch, l.H * l.W, l.C, l.groups, P->cus, launch);
+    case K_ATTN: {
+        if (launch_roles(P, l, batch)[launch] == L_ROTARY) return rotary_name(P->dtype);
+        return attention_name(P->dtype, layer_attention(l, P->dtype, batch, nullptr, nullptr,
+                                                        nullptr), P->cus, launch - rotates(l));
+    }
     default: return gap_name(P->dtype);
     }
 }
@@ -569,7 +661,7 @@ std::string record_name(const ppipe_partition* P, const LayerRT& l, int batch, i
 
 // Algorithmic work of one launch: FLOPs, and the layer's input, weight,
 // output and residual bytes each counted once.  In a multi-launch layer the
-// first launch owns the input (the GEMM also the weights and FLOPs) and the
+// first launch owns the input (the GEMM, norm or attention also the weights and FLOPs) and the
 // last launch the output and residual; a split-K reduction in between owns
 // nothing.  A block's one launch owns the FLOPs and weights of its three
 // layers, the first one's input and the last one's output and residual.
@@ -587,12 +679,13 @@ void launch_work(const ppipe_partition* P, const LayerRT& l, int batch, int laun
     const double b = batch;
     const double out_bytes = b * (double)l.out_bytes_b1 *
                              (l.softmax ? 4.0 / dtype_size(P->dtype) : 1.0);
-    const std::vector<int> roles = launch_roles(l, batch);
+    const std::vector<int> roles = launch_roles(P, l, batch);
     const int n = (int)roles.size(), role = roles[launch];
-    *flops = (role == L_GEMM || role == L_OTHER) ? b * l.flops_b1 : 0.0;
+    const bool main = role == L_GEMM || role == L_OTHER || role == L_NORM || role == L_ATTN;
+    *flops = main ? b * l.flops_b1 : 0.0;
     double by = 0.0;
     if (launch == 0) by += b * l.in_bytes_b1;
-    if (role == L_GEMM || role == L_OTHER) by += l.param_bytes;
+    if (main) by += l.param_bytes;
     if (launch == n - 1) by += out_bytes + b * l.res_bytes_b1;
     *bytes = by;
 }
@@ -715,7 +808,7 @@ hipError_t enqueue_layer(const ppipe_partition* P, const LayerRT& l, int batch, 
     switch (l.kind) {
     case K_GEMM: {
         const Plan& p = l.plans[batch - 1];
-        const std::vector<int> roles = launch_roles(l, batch);
+        const std::vector<int> roles = launch_roles(P, l, batch);
         auto want = [&](int i) { return only < 0 || only == i; };
         int li = 0;
         const bool pad = pads_input(l, p);
@@ -776,6 +869,26 @@ hipError_t enqueue_layer(const ppipe_partition* P, const LayerRT& l, int batch, 
                            l.pad, s);
         if (hook) hook->after(l, 0, s);
         return e;
+    case K_NORM:
+    case K_ATTN: {
+        // an attention layer's scratch: rotated heads, then its partial results
+        const int n = (int)launch_roles(P, l, batch).size(), rot = l.kind == K_ATTN && rotates(l);
+        for (int i = 0; i < n && e == hipSuccess; ++i) {
+            if (only >= 0 && only != i) continue;
+            if (hook) hook->before(l, i, s);
+            if (l.kind == K_NORM)
+                e = launch_group_norm(P->dtype, norm_args(l, batch, x, y), W.ws, P->cus, i, s);
+            else if (rot && i == 0)
+                e = launch_rotary(P->dtype, rotary_args(rotary_desc(l, P->dtype, batch), x, l.pos,
+                                                        W.ws), s);
+            else
+                e = launch_attention(P->dtype, layer_attention(l, P->dtype, batch, x, y, W.ws),
+                                     (uint8_t*)W.ws + rotated_bytes(l, P->dtype, batch), P->cus,
+                                     i - rot, s);
+            if (hook) hook->after(l, i, s);
+        }
+        return e;
+    }
     default:
         if (hook) hook->before(l, 0, s);
         e = launch_gap(P->dtype, x, y, batch, l.H * l.W, l.C, s);
@@ -919,7 +1032,8 @@ float median_of(std::vector<float> v)
     return n % 2 ? v[n / 2] : 0.5f * (v[n / 2 - 1] + v[n / 2]);
 }
 
-int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int dt)
+int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int dt,
+          const ppipe_attention_layer* att, int n_att)
 {
     const int n = d->n_layers;
     const int esz = dtype_size(dt);
@@ -960,6 +1074,13 @@ int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int
             if (ld.c_out < 1)
                 return fail(PPIPE_E_INVALID, who + ": fc c_out < 1");
             sh[i] = {ld.c_out, 1, 1};
+        } else if (ld.op == PPIPE_OP_GROUPNORM || ld.op == PPIPE_OP_ATTENTION) {
+            if (ld.c_in != x.c || ld.c_out < 1 ||
+                (ld.op == PPIPE_OP_GROUPNORM && ld.c_out != ld.c_in))
+                return fail(PPIPE_E_INVALID, who + ": c_in " + std::to_string(ld.c_in) +
+                                                 " must be the producer's channels " +
+                                                 std::to_string(x.c) + ", and a norm's c_out");
+            sh[i] = {ld.c_out, x.h, x.w};
         } else {
             return fail(PPIPE_E_INVALID, who + ": unknown op " + std::to_string(ld.op));
         }
@@ -1007,7 +1128,8 @@ int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int
         l.name = ld.name && ld.name[0] ? std::string(ld.name) : "layer" + std::to_string(i);
         l.k = ld.k; l.stride = ld.stride; l.pad = ld.pad; l.groups = ld.groups;
         l.H = x.h; l.W = x.w; l.C = x.c; l.Ho = o.h; l.Wo = o.w; l.Co = o.c;
-        if (ld.act < PPIPE_ACT_NONE || ld.act > PPIPE_ACT_RELU6)
+        if (ld.act < PPIPE_ACT_NONE ||
+            ld.act > (ld.op == PPIPE_OP_GROUPNORM ? PPIPE_ACT_GELU : PPIPE_ACT_RELU6))
             return fail(PPIPE_E_INVALID, who + ": unknown activation");
         l.out_bytes_b1 = (int64_t)o.c * o.h * o.w * esz;
         l.in_bytes_b1 = (double)x.c * x.h * x.w * esz;
@@ -1081,6 +1203,55 @@ int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int
                 return fail(PPIPE_E_UNSUPPORTED, who + ": window larger than 32");
             l.flops_b1 = 2.0 * o.c * o.h * o.w * (double)(l.KH * l.KW * x.c);
             l.param_bytes = (double)o.c * l.KH * l.KW * x.c * esz + 8.0 * o.c;
+        } else if (ld.op == PPIPE_OP_GROUPNORM) {
+            l.kind = K_NORM;
+            l.eps = ld.bn_eps > 0.0f ? ld.bn_eps : 1e-5f;
+            const int rc = check_group_norm(dt, P->max_batch, (int64_t)x.h * x.w, x.c, ld.groups,
+                                            l.eps, ld.act, who + ": ");
+            if (rc != PPIPE_OK) return rc;
+            l.flops_b1 = 8.0 * x.c * x.h * x.w;
+            l.param_bytes = 8.0 * x.c;
+        } else if (ld.op == PPIPE_OP_ATTENTION) {
+            l.kind = K_ATTN;
+            const ppipe_attention_layer* found = nullptr;
+            for (int q = 0; q < n_att; ++q)
+                if (att[q].layer == i) {
+                    if (found)
+                        return fail(PPIPE_E_INVALID, who + ": described twice");
+                    found = &att[q];
+                }
+            if (!found)
+                return fail(PPIPE_E_INVALID, who + ": attention needs its ppipe_attention_layer "
+                                                   "(ppipe_partition_create_attention)");
+            l.att = *found;
+            ppipe_attention_layer& t = l.att;
+            if (t.heads < 1 || t.kv_heads < 1 || ld.c_out % t.heads ||
+                (int64_t)ld.c_in * t.heads !=
+                    (int64_t)ld.c_out * ((int64_t)t.heads + 2 * (int64_t)t.kv_heads))
+                return fail(PPIPE_E_INVALID, who + ": channels must be (heads + 2 kv_heads) x "
+                                                   "head_dim in and heads x head_dim out");
+            const int64_t hw = (int64_t)x.h * x.w;
+            if (ld.act != PPIPE_ACT_NONE)
+                return fail(PPIPE_E_INVALID, who + ": attention takes no activation");
+            if (t.prefix < 0 || (t.prefix > 0 && !t.causal))
+                return fail(PPIPE_E_INVALID, who + ": a prefix is for causal masks, and not negative");
+            if (hw > ATTENTION_MAX_LEN)
+                return fail(PPIPE_E_UNSUPPORTED, who + ": attention of this size is not supported");
+            if (t.scale == 0.0f) t.scale = (float)(1.0 / std::sqrt((double)(ld.c_out / t.heads)));
+            if (t.rotary_base == 0.0) t.rotary_base = 10000.0;
+            int rc = check_attention(attention_desc(l, dt, P->max_batch), who + ": ");
+            if (rc != PPIPE_OK) return rc;
+            if ((t.rotary_pairs[0] || t.rotary_pairs[1]) &&
+                (rc = check_rotary(rotary_desc(l, dt, P->max_batch), who + ": ")) != PPIPE_OK)
+                return rc;
+            double pairs = (double)hw * hw;
+            if (t.causal) {
+                pairs = 0;
+                for (int64_t q = 0; q < hw; ++q)
+                    pairs += (double)std::max(q + 1, std::min<int64_t>(t.prefix, hw));
+            }
+            l.flops_b1 = 4.0 * ld.c_out * pairs;
+            l.param_bytes = (t.slopes ? 4.0 * t.heads : 0.0);
         } else if (ld.op == PPIPE_OP_MAXPOOL) {
             if (x.c % epv)
                 return fail(PPIPE_E_UNSUPPORTED, who + ": maxpool needs C % " +
@@ -1107,7 +1278,15 @@ int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int
             l.w_off = total; total = align(total + (size_t)l.Co * l.Kpad * esz);
         } else if (l.kind == K_DW) {
             l.w_off = total; total = align(total + (size_t)l.k * l.k * l.Co * esz);
-        } else {
+        } else if (l.kind == K_ATTN) {
+            const size_t map = (size_t)l.H * l.W * 2 * sizeof(int);
+            l.scale_off = total; total = align(total + (size_t)l.att.heads * 4);   // slopes
+            l.pos_off = total; total = align(total + map);
+            if (l.att.causal) {
+                l.spans_off = total; total = align(total + map);
+            }
+            continue;
+        } else if (l.kind != K_NORM) {
             continue;
         }
         l.scale_off = total; total = align(total + (size_t)l.Co * 4);
@@ -1118,8 +1297,27 @@ int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int
     }
     std::vector<uint8_t> blob(std::max<size_t>(total, 256), 0);
     for (LayerRT& l : P->L) {
-        if (l.kind != K_GEMM && l.kind != K_DW) continue;
         const ppipe_layer_desc& ld = d->layers[l.index];
+        if (l.kind == K_NORM) {
+            for (int c = 0; c < l.Co; ++c) {
+                ((float*)&blob[l.scale_off])[c] = ld.bn_gamma ? ld.bn_gamma[c] : 1.0f;
+                ((float*)&blob[l.bias_off])[c] = ld.bn_beta ? ld.bn_beta[c] : 0.0f;
+            }
+        } else if (l.kind == K_ATTN) {
+            if (l.att.slopes)
+                std::memcpy(&blob[l.scale_off], l.att.slopes, (size_t)l.att.heads * 4);
+            const int hw = l.H * l.W;
+            for (int i = 0; i < hw; ++i) {
+                int* pos = (int*)&blob[l.pos_off] + 2 * (size_t)i;
+                pos[0] = i / l.W;
+                pos[1] = i % l.W;
+                if (!l.att.causal) continue;
+                int* span = (int*)&blob[l.spans_off] + 2 * (size_t)i;
+                span[0] = 0;
+                span[1] = std::max(i + 1, std::min(l.att.prefix, hw));
+            }
+        }
+        if (l.kind != K_GEMM && l.kind != K_DW) continue;
         if (l.kind == K_GEMM) {
             if (l.op == PPIPE_OP_CONV) {
                 // OIHW [co][ci][kh][kw] -> [co][(kh * KW + kw) * cpad + ci]
@@ -1274,6 +1472,8 @@ int build(ppipe_partition* P, const ppipe_model_desc* d, int begin, int end, int
     // ---- kernel plans for every batch, logits workspace ----
     size_t ws = 0;
     for (LayerRT& l : P->L) {
+        if (l.kind == K_NORM || l.kind == K_ATTN)
+            for (int b = 1; b <= P->max_batch; ++b) ws = std::max(ws, layer_scratch(P, l, b));
         if (l.kind != K_GEMM) continue;
         l.plans.resize(P->max_batch);
         for (int b = 1; b <= P->max_batch; ++b) {
@@ -1331,7 +1531,12 @@ int allocate(ppipe_partition* P)
     if (e != hipSuccess) return fail(PPIPE_E_HIP, hip_msg("hipMemcpy(weights)", e));
     std::vector<uint8_t>().swap(P->host_blob);
     for (LayerRT& l : P->L) {
-        if (l.kind != K_GEMM && l.kind != K_DW) continue;
+        if (l.kind == K_ATTN) {
+            l.scale = (float*)((uint8_t*)P->wblob + l.scale_off);
+            l.pos = (const int*)((uint8_t*)P->wblob + l.pos_off);
+            if (l.att.causal) l.spans = (const int*)((uint8_t*)P->wblob + l.spans_off);
+        }
+        if (l.kind != K_GEMM && l.kind != K_DW && l.kind != K_NORM) continue;
         l.w = (uint8_t*)P->wblob + l.w_off;
         l.scale = (float*)((uint8_t*)P->wblob + l.scale_off);
         l.bias = (float*)((uint8_t*)P->wblob + l.bias_off);
@@ -1505,6 +1710,7 @@ void scratch_need(const ppipe_partition* P, int batch, size_t* ws_bytes, size_t*
     size_t ws = 0, pad = 0;
     const int esz = dtype_size(P->dtype);
     for (const LayerRT& l : P->L) {
+        ws = std::max(ws, layer_scratch(P, l, batch));
         if (l.kind != K_GEMM) continue;
         const Plan& p = l.plans[batch - 1];
         const size_t M = (size_t)batch * l.Ho * l.Wo;
@@ -1552,7 +1758,8 @@ int share_cus(int parts)
 
 ppipe_partition* create_partition(const ppipe_model_desc* desc, int32_t layer_begin,
                                   int32_t layer_end, int32_t dtype, const ppipe_tuning* tuning,
-                                  int32_t parts)
+                                  int32_t parts, const ppipe_attention_layer* attention = nullptr,
+                                  int32_t n_attention = 0)
 {
     g_err.clear();
     g_status = 0;
@@ -1572,6 +1779,17 @@ ppipe_partition* create_partition(const ppipe_model_desc* desc, int32_t layer_be
     if (!desc || !desc->layers || desc->n_layers < 1) {
         fail(PPIPE_E_INVALID, "model description is empty");
         return nullptr;
+    }
+    if (n_attention < 0 || (n_attention > 0 && !attention)) {
+        fail(PPIPE_E_INVALID, "attention layers: null or a negative number");
+        return nullptr;
+    }
+    for (int i = 0; i < n_attention; ++i) {
+        const int q = attention[i].layer;
+        if (q < 0 || q >= desc->n_layers || desc->layers[q].op != PPIPE_OP_ATTENTION) {
+            fail(PPIPE_E_INVALID, "layer " + std::to_string(q) + " is no attention layer");
+            return nullptr;
+        }
     }
     if (dtype < PPIPE_F32 || dtype > PPIPE_BF16) {
         fail(PPIPE_E_INVALID, "unknown dtype " + std::to_string(dtype));
@@ -1599,7 +1817,8 @@ ppipe_partition* create_partition(const ppipe_model_desc* desc, int32_t layer_be
     P->cus = share_cus(parts);
     // host-side validation and packing first: a bad description fails
     // without touching the device
-    if (build(P, desc, layer_begin, layer_end, dtype) != PPIPE_OK || allocate(P) != PPIPE_OK) {
+    if (build(P, desc, layer_begin, layer_end, dtype, attention, n_attention) != PPIPE_OK ||
+        allocate(P) != PPIPE_OK) {
         std::string msg = g_err;
         const int st = g_status;
         release(P);
@@ -1631,6 +1850,16 @@ ppipe_partition* ppipe_partition_create_on_share(const ppipe_model_desc* desc,
                                                  int32_t dtype, int32_t parts)
 {
     return create_partition(desc, layer_begin, layer_end, dtype, nullptr, parts);
+}
+
+ppipe_partition* ppipe_partition_create_attention(const ppipe_model_desc* desc,
+                                                  int32_t layer_begin, int32_t layer_end,
+                                                  int32_t dtype,
+                                                  const ppipe_attention_layer* attention,
+                                                  int32_t n_attention, int32_t parts)
+{
+    return create_partition(desc, layer_begin, layer_end, dtype, nullptr, parts, attention,
+                            n_attention);
 }
 
 void ppipe_partition_destroy(ppipe_partition* h)
@@ -2120,11 +2349,12 @@ int ppipe_layer_info(const ppipe_partition* h, int32_t index, int32_t batch,
     info->flops_b1 = l.flops_b1;
     info->act_bytes_b1 = l.in_bytes_b1 + l.res_bytes_b1 + (double)info->out_bytes_b1;
     info->param_bytes = l.param_bytes;
-    // name the GEMM launch of a GEMM layer, not its channel-pad prologue
-    const std::vector<int> roles = launch_roles(l, batch);
+    // name the GEMM launch of a GEMM layer, not its channel-pad prologue (and the
+    // norm of a group norm, the attention of an attention layer)
+    const std::vector<int> roles = launch_roles(h, l, batch);
     int main_launch = 0;
     for (size_t i = 0; i < roles.size(); ++i)
-        if (roles[i] == L_GEMM) main_launch = (int)i;
+        if (roles[i] == L_GEMM || roles[i] == L_NORM || roles[i] == L_ATTN) main_launch = (int)i;
     std::string k = launch_name(h, l, batch, main_launch);
     if (l.kind == K_GEMM) {
         const Plan& p = l.plans[batch - 1];
