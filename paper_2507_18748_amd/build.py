@@ -10,7 +10,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libppipe.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["conv_gemm.hip", "split_gemm.hip", "fused_block.hip", "pointwise.hip", "mem_kernels.hip",
-           "group_norm.hip", "rotary.hip", "attention.hip", "operators.hip", "runtime.hip", "batcher.cpp"]
+           "group_norm.hip", "rotary.hip", "attention.hip", "attention_f32.hip",
+           "attention_f16.hip", "attention_bf16.hip", "operators.hip", "runtime.hip", "batcher.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

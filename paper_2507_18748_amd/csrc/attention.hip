@@ -1,10 +1,18 @@
 // Attention over [batch][token][head][dim] tensors by strides (see
 // ppipe_attention_desc), and the spans of keys that its queries see.
 //
-// One wave takes one query of one head and walks its visible keys 64 at a
-// time with a running maximum and sum: a lane scores one key, then each lane
-// adds the values of its elements of the head.
-#include "kernels.h"
+//   o_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c s_ij - M_i)
+//
+// in one pass over the keys with a running maximum M and sum.  The scores are
+// computed transposed, S^T = K Q^T, so that a lane holds one query's scores
+// (half of a tile's keys, the other half wave the other half): maximum and sum
+// stay in the lane, and the weights are already the right operand of
+// O^T = V^T P^T if the keys of V^T come in the same order, which the transposing
+// LDS reads give for 16-bit types and plain reads for fp32.
+//
+// Rows: the queries of all heads that share a key head, (token, head) with the
+// head fastest, 32 to a wave, so that few tokens with many heads fill a tile.
+#include "attention_device.h"
 
 namespace ppipe {
 namespace {
@@ -38,61 +46,68 @@ __global__ void __launch_bounds__(256) attention_spans_kernel(SpansArgs a)
     a.spans[2 * i + 1] = end;
 }
 
+// Parts of the splits brought to one maximum, added in split order and
+// normalised; a thread takes four elements of a row.
 template <typename T>
-__global__ void __launch_bounds__(256) attention_kernel(AttentionArgs a)
+__global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a, AttentionPlan p)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    const int lane = threadIdx.x % 64;
-    if (row >= (int64_t)a.N * a.Lq * a.H) return;
-    const int h = (int)(row % a.H);
-    const int64_t t = row / a.H;
-    const int n = (int)(t / a.Lq), i = (int)(t % a.Lq), hk = h / (a.H / a.Hk);
-    const T* q = (const T*)a.q + n * a.qs[0] + i * a.qs[1] + h * a.qs[2];
-    const T* k = (const T*)a.k + n * a.ks[0] + hk * a.ks[2];
-    const T* v = (const T*)a.v + n * a.vs[0] + hk * a.vs[2];
-    T* out = (T*)a.out + n * a.os[0] + i * a.os[1] + h * a.os[2];
-    int lo = 0, hi = a.Lk;
-    if (a.spans) {
-        lo = max(0, a.spans[n * a.sps + 2 * (int64_t)i]);
-        hi = min(a.Lk, a.spans[n * a.sps + 2 * (int64_t)i + 1]);
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)a.N * a.Hk * p.rows;
+    const int quads = a.d / 4;
+    const int64_t row = x / quads;
+    const int e = 4 * (int)(x - row * quads);
+    if (row >= all) return;
+    float m = -INFINITY;
+    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, p.ml[(s * all + row) * 2]);
+    float w = 0.0f;
+    float4 sum = make_float4(0, 0, 0, 0);
+    for (int s = 0; s < p.splits; ++s) {
+        const float ms = p.ml[(s * all + row) * 2];
+        if (ms == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(ms - m);
+        const float4 v = *(const float4*)(p.part + (s * all + row) * a.d + e);
+        w += p.ml[(s * all + row) * 2 + 1] * f;
+        sum.x += v.x * f; sum.y += v.y * f; sum.z += v.z * f; sum.w += v.w * f;
     }
-    float m = -INFINITY, l = 0.0f, acc[4] = {};
-    for (int j0 = lo; j0 < hi; j0 += 64) {
-        const int j = j0 + lane;
-        float s = -INFINITY;
-        if (j < hi) {
-            float dot = 0.0f;
-            for (int e = 0; e < a.d; ++e) dot += (float)q[e] * (float)k[j * a.ks[1] + e];
-            s = dot * a.scale;
-            if (a.cap > 0.0f) s = a.cap * tanhf(s / a.cap);
-            if (a.slopes) {
-                uint32_t dist = 0;
-                for (int x = 0; x < a.A; ++x) {
-                    const int p = a.qpos[n * a.qps + (int64_t)i * a.A + x];
-                    const int r = a.kpos[n * a.kps + (int64_t)j * a.A + x];
-                    dist += (uint32_t)max(p, r) - (uint32_t)min(p, r);
-                }
-                s -= a.slopes[h] * (float)dist;
-            }
-        }
-        float top = s;
-        for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-        const float mn = fmaxf(m, top), base = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = expf(m - base), p = expf(s - base);
-        float sum = p;
-        for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
-        l = l * alpha + sum;
-        m = mn;
-        for (int x = 0; x < 4; ++x) acc[x] *= alpha;
-        for (int jj = 0; jj < 64 && j0 + jj < hi; ++jj) {
-            const float pj = __shfl(p, jj);
-            for (int x = 0; x < 4; ++x)
-                if (lane + 64 * x < a.d)
-                    acc[x] += pj * (float)v[(j0 + jj) * a.vs[1] + lane + 64 * x];
-        }
-    }
-    for (int x = 0; x < 4; ++x)
-        if (lane + 64 * x < a.d) out[lane + 64 * x] = (T)(l == 0.0f ? 0.0f : acc[x] / l);
+    const int64_t group = row / p.rows;
+    const int r = (int)(row - group * p.rows), G = a.H / a.Hk, i = r / G;
+    const int n = (int)(group / a.Hk), h = (int)(group - (int64_t)n * a.Hk) * G + r - i * G;
+    T* y = (T*)a.out + n * a.os[0] + i * a.os[1] + h * a.os[2] + e;
+    const float inv = w == 0.0f ? 0.0f : 1.0f / w;
+    Vec4<T>::store(y, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+}
+
+// Rows of one key head up to 32: the waves of a block split the keys, and the
+// keys are split further among blocks until the chip is filled; each part keeps at
+// least 512 keys.
+AttentionChoice choose(int, const AttentionArgs& a, int cus)
+{
+    AttentionChoice c;
+    const int64_t rows = (int64_t)a.Lq * (a.H / a.Hk), groups = (int64_t)a.N * a.Hk;
+    c.splitk = rows <= 32;
+    const int per = c.splitk ? 32 : 128;
+    c.tiles = (int)((rows + per - 1) / per);
+    c.splits = 1;
+    while (c.splitk && c.splits < 64 && groups * c.tiles * c.splits < 2 * cus &&
+           a.Lk / (c.splits * 2) >= 512)
+        c.splits *= 2;
+    c.blocks = groups * c.tiles * c.splits;
+    return c;
+}
+
+AttentionPlan plan_of(const AttentionArgs& a, const AttentionChoice& c, void* ws)
+{
+    AttentionPlan p;
+    p.rows = a.Lq * (a.H / a.Hk);
+    p.tiles = c.tiles;
+    p.splits = c.splits;
+    const bool extra = a.cap > 0.0f || a.slopes;
+    p.sign = a.scale == 0.0f ? 0 : a.scale < 0.0f ? -1 : 1;
+    p.pre = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
+    p.c = (float)(1.4426950408889634 * (extra ? 1.0 : (double)p.pre));
+    const int64_t all = (int64_t)a.N * a.Hk * p.rows;
+    p.part = (float*)ws;
+    p.ml = ws ? (float*)ws + c.splits * all * a.d : nullptr;
+    return p;
 }
 
 }  // namespace
@@ -104,22 +119,41 @@ hipError_t launch_attention_spans(const SpansArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t attention_workspace(int, const AttentionArgs&, int) { return 0; }
-int attention_launches(int, const AttentionArgs&, int) { return 1; }
-const char* attention_name(int dt, const AttentionArgs&, int, int)
+size_t attention_workspace(int dt, const AttentionArgs& a, int cus)
 {
-    return dt == DT_F32 ? "attention<f32>" : dt == DT_F16 ? "attention<f16>" : "attention<bf16>";
+    const AttentionChoice c = choose(dt, a, cus);
+    return c.splits > 1 ? (size_t)c.splits * a.N * a.Lq * a.H * (a.d + 2) * 4 : 0;
 }
 
-hipError_t launch_attention(int dt, const AttentionArgs& a, void*, int, int, hipStream_t s)
+int attention_launches(int dt, const AttentionArgs& a, int cus)
 {
-    const dim3 grid((uint32_t)(((int64_t)a.N * a.Lq * a.H + 3) / 4)), block(256);
-    if (dt == DT_F32)
-        PPIPE_LAUNCH(attention_kernel<float>, grid, block, 0, s, a);
-    else if (dt == DT_F16)
-        PPIPE_LAUNCH(attention_kernel<_Float16>, grid, block, 0, s, a);
-    else
-        PPIPE_LAUNCH(attention_kernel<__bf16>, grid, block, 0, s, a);
+    return choose(dt, a, cus).splits > 1 ? 2 : 1;
+}
+
+const char* attention_name(int dt, const AttentionArgs&, int, int launch)
+{
+    static const char* names[2][3] = {
+        {"attention<f32>", "attention<f16>", "attention<bf16>"},
+        {"attention_join<f32>", "attention_join<f16>", "attention_join<bf16>"}};
+    return names[launch][dt];
+}
+
+hipError_t launch_attention(int dt, const AttentionArgs& a, void* ws, int cus, int launch,
+                            hipStream_t s)
+{
+    const AttentionChoice c = choose(dt, a, cus);
+    const AttentionPlan p = plan_of(a, c, ws);
+    if (launch == 1) {
+        const int64_t n = (int64_t)a.N * a.Lq * a.H * (a.d / 4);
+        const dim3 grid((uint32_t)((n + 255) / 256)), block(256);
+        if (dt == DT_F32) PPIPE_LAUNCH(attention_join_kernel<float>, grid, block, 0, s, a, p);
+        else if (dt == DT_F16) PPIPE_LAUNCH(attention_join_kernel<_Float16>, grid, block, 0, s, a, p);
+        else PPIPE_LAUNCH(attention_join_kernel<__bf16>, grid, block, 0, s, a, p);
+        return hipGetLastError();
+    }
+    if (dt == DT_F32) launch_attention_f32(a, p, c, s);
+    else if (dt == DT_F16) launch_attention_f16(a, p, c, s);
+    else launch_attention_bf16(a, p, c, s);
     return hipGetLastError();
 }
 

@@ -1,0 +1,647 @@
+// Device side of the attention kernels: tile loads, matrix instructions and
+// the pass over the keys with a running maximum and sum.
+#pragma once
+#include "gemm_device.h"
+
+namespace ppipe {
+
+typedef float accx16 __attribute__((ext_vector_type(16)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+// What a launch adds to the call's arguments.
+struct AttentionPlan {
+    int rows;          // query rows of one key head: Lq * (H / Hk)
+    int tiles;         // row tiles of one key head
+    int splits;        // key ranges per row tile
+    float c;           // scores in powers of two: c * (q . k), or log2(e) after cap and bias
+    float pre;         // with cap or bias: the scale itself
+    int sign;          // 0: q is read as zeros, -1: with its sign turned
+    float* part;       // [splits][N * Hk * rows][d] sums and [..][2] maxima and weights
+    float* ml;
+};
+
+// How a call is cut into blocks.
+struct AttentionChoice {
+    bool splitk;       // the waves of a block take keys, not rows
+    int tiles, splits;
+    int64_t blocks;
+};
+void launch_attention_f32(const AttentionArgs& a, const AttentionPlan& p, const AttentionChoice& c,
+                          hipStream_t s);
+void launch_attention_f16(const AttentionArgs& a, const AttentionPlan& p, const AttentionChoice& c,
+                          hipStream_t s);
+void launch_attention_bf16(const AttentionArgs& a, const AttentionPlan& p, const AttentionChoice& c,
+                           hipStream_t s);
+
+// One 32 x 32 block of products over 16 bytes of k per lane (16-bit types:
+// 16 of k, half a wave each 8; fp32: 8 of k, half a wave each 4, in four
+// instructions).  Lane l gives row or column l % 32; of the result it holds
+// column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 in register i.
+template <typename T> struct Mfma32;
+template <> struct Mfma32<_Float16> {
+    static __device__ __forceinline__ void step(const uint4& a, const uint4& b, accx16& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a),
+                                                   __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mfma32<__bf16> {
+    static __device__ __forceinline__ void step(const uint4& a, const uint4& b, accx16& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mfma32<float> {
+    static __device__ __forceinline__ void step(const uint4& a, const uint4& b, accx16& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+    }
+};
+
+// One 4-byte load per lane into LDS (see dma16).
+__device__ __forceinline__ void dma4(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :: "s"(lds), "v"(voff), "s"(r) : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+// Four 16-bit values of one column: lane l of each 16 names the 8 bytes of row
+// l / 4, columns 4 (l % 4) of a 4 x 16 block and receives column l's four rows.
+__device__ __forceinline__ uint2 lds_read_columns(uint32_t addr)
+{
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) shortx4*)(uintptr_t)addr));
+}
+
+// Maximum of the two half waves.
+__device__ __forceinline__ float half_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ int wave_min(int v)
+{
+    for (int m = 32; m; m >>= 1) v = min(v, __shfl_xor(v, m));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max(int v)
+{
+    for (int m = 32; m; m >>= 1) v = max(v, __shfl_xor(v, m));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 lds_read16(uint32_t addr)
+{
+    return __builtin_bit_cast(uint4, *(const __attribute__((address_space(3))) uintx4*)(uintptr_t)addr);
+}
+__device__ __forceinline__ float lds_read_f32(uint32_t addr)
+{
+    return *(const __attribute__((address_space(3))) float*)(uintptr_t)addr;
+}
+
+// |a - b| + c of integers whose sign bits were turned.
+__device__ __forceinline__ uint32_t sad(uint32_t a, uint32_t b, uint32_t c)
+{
+    return max(a, b) - min(a, b) + c;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    const T e[2] = {(T)a, (T)b};
+    uint32_t u;
+    __builtin_memcpy(&u, e, 4);
+    return u;
+}
+
+// SPLITK: the waves of a block share one tile of rows and take key tiles in
+// turn, each with LDS of its own and no barrier (few rows, long caches: bound
+// by the bytes in flight).  Otherwise they take rows of their own and share
+// the key tiles.
+template <typename T, int DP, int QT, bool SPLITK> struct AttentionTile {
+    static constexpr int ESZ = (int)sizeof(T);
+    static constexpr int CH = DP * ESZ / 16;                    // 16-byte vectors of a row
+    static constexpr int BK = SPLITK || 4 * 64 * DP * ESZ > 131072 ? 32 : 64;
+    static constexpr int KT = BK / 32;
+    static constexpr int POS = 64 * 3 * 4;                      // key positions of a tile
+    static constexpr int STAGE = 2 * BK * DP * ESZ + POS;
+    static constexpr int NW = !SPLITK || 8 * STAGE <= 160 * 1024 ? 4 : 4 * STAGE <= 160 * 1024 ? 2 : 1;
+    static constexpr int STAGES = 2 * (SPLITK ? NW : 1);
+    static constexpr int JOIN = SPLITK && NW > 1 ? NW * 32 * (DP + 2) * 4 : 0;
+    static constexpr int LDS = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
+    static constexpr int WAVES = ESZ == 2 && DP <= 128 && QT == 1 && !SPLITK ? 2 : 1;   // per SIMD
+    static constexpr int ROWS = SPLITK ? 32 : 32 * QT * NW;     // rows of a block
+    static constexpr int NI = BK * CH / 64;                     // wave loads of a K or V tile
+    static constexpr int NL = SPLITK ? NI : NI / NW;            // of them, one wave's
+    // Row r keeps vector c of K at c ^ kswz(r): the 8 rows that a fragment read
+    // takes at once lie in different banks.  Of V, 16-bit: the 4 rows of a
+    // transposing read do.
+    static __device__ __forceinline__ int kswz(int r) { return CH % 8 == 0 ? r & 7 : (r >> 1) & 3; }
+    static __device__ __forceinline__ int vswz(int r)
+    {
+        return ESZ == 4 ? 0 : CH % 8 == 0 ? (r & 3) << 1 : ((r >> 1) & 1) << 1;
+    }
+};
+
+template <typename T, int DP, int QT, bool SPLITK, bool EXTRA>
+__global__ void __launch_bounds__((AttentionTile<T, DP, QT, SPLITK>::NW * 64),
+                                  (AttentionTile<T, DP, QT, SPLITK>::WAVES))
+attention_kernel(AttentionArgs a, AttentionPlan p)
+{
+    using TL = AttentionTile<T, DP, QT, SPLITK>;
+    constexpr int ESZ = TL::ESZ, CH = TL::CH, BK = TL::BK, KT = TL::KT, NW = TL::NW, NL = TL::NL;
+    constexpr int DT = DP / 32, RB = DP * ESZ, KB = BK * RB;
+    constexpr int EPV = 16 / ESZ;
+    __shared__ __align__(1024) uint8_t lds[TL::LDS];
+    __shared__ int range[2 * NW];
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int col = lane % 32, half = lane / 32;
+    // blocks of one key head lie on one XCD, the later rows (more keys under a
+    // causal mask) first
+    const uint32_t per = gridDim.x / NUM_XCD, rem = gridDim.x % NUM_XCD;
+    const uint32_t xcd = blockIdx.x % NUM_XCD;
+    uint32_t lin = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / NUM_XCD;
+    const int split = lin % (uint32_t)p.splits;
+    lin /= (uint32_t)p.splits;
+    const int tile = p.tiles - 1 - (int)(lin % (uint32_t)p.tiles);
+    const int group = (int)(lin / (uint32_t)p.tiles);          // n * Hk + hk
+    const int n = group / a.Hk, hk = group - n * a.Hk, G = a.H / a.Hk;
+
+    // ---- this lane's rows: query, span, bias ----
+    const int row0 = tile * TL::ROWS + (SPLITK ? 0 : wave * 32 * QT);
+    uint4 q[QT][CH / 2];
+    int lo[QT], hi[QT];
+    float slope[QT];
+    uint32_t qp[QT][3];
+    int wlo = 0x7fffffff, whi = 0, wlo_max = 0, whi_min = 0x7fffffff;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int r = row0 + 32 * t + col;
+        const bool ok = r < p.rows;
+        const int i = ok ? r / G : 0, h = hk * G + (ok ? r - i * G : 0);
+        const T* qr = (const T*)a.q + n * a.qs[0] + i * a.qs[1] + h * a.qs[2];
+#pragma unroll
+        for (int c = 0; c < CH / 2; ++c) {
+            const int e = (2 * c + half) * EPV;
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (ok && e < a.d && p.sign) u = *(const uint4*)(qr + e);
+            if (p.sign < 0) {
+                const uint32_t m = ESZ == 4 ? 0x80000000u : 0x80008000u;
+                u.x ^= m; u.y ^= m; u.z ^= m; u.w ^= m;
+            }
+            q[t][c] = u;
+        }
+        lo[t] = 0;
+        hi[t] = ok ? a.Lk : 0;
+        if (ok && a.spans) {
+            const int* sp = a.spans + n * a.sps + 2 * (int64_t)i;
+            lo[t] = max(sp[0], 0);
+            hi[t] = min(sp[1], a.Lk);
+        }
+        if (hi[t] <= lo[t]) lo[t] = hi[t] = 0;
+        if (hi[t] > lo[t]) {
+            wlo = min(wlo, lo[t]);
+            whi = max(whi, hi[t]);
+        }
+        if (ok) {
+            wlo_max = max(wlo_max, lo[t]);
+            whi_min = min(whi_min, hi[t]);
+        }
+        if constexpr (EXTRA) {
+            slope[t] = a.slopes && ok ? a.slopes[h] : 0.0f;
+#pragma unroll
+            for (int x = 0; x < 3; ++x)
+                qp[t][x] = a.slopes && ok && x < a.A
+                               ? (uint32_t)a.qpos[n * a.qps + (int64_t)i * a.A + x] ^ 0x80000000u : 0u;
+        }
+    }
+    wlo = wave_min(wlo);
+    whi = wave_max(whi);
+    wlo_max = wave_max(wlo_max);
+    whi_min = wave_min(whi_min);
+
+    // ---- the block's keys, and this split's part of them in whole tiles ----
+    int kbeg = wlo, kend = whi;
+    if constexpr (!SPLITK) {
+        if (lane == 0) {
+            range[wave] = wlo;
+            range[NW + wave] = whi;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            kbeg = min(kbeg, range[w]);
+            kend = max(kend, range[NW + w]);
+        }
+        kbeg = __builtin_amdgcn_readfirstlane(kbeg);
+        kend = __builtin_amdgcn_readfirstlane(kend);
+    }
+    int ntiles = kend > kbeg ? (kend - kbeg + BK - 1) / BK : 0;
+    if (p.splits > 1) {
+        const int each = (ntiles + p.splits - 1) / p.splits;
+        const int first = min(split * each, ntiles);
+        ntiles = min(each, ntiles - first);
+        kbeg += first * BK;
+        kend = min(kend, kbeg + ntiles * BK);
+    }
+    if constexpr (SPLITK) {                    // tiles wave, wave + NW, ... are this wave's
+        kbeg += wave * BK;
+        ntiles = ntiles > wave ? (ntiles - wave + NW - 1) / NW : 0;
+    }
+    constexpr int STEP = SPLITK ? NW * BK : BK;
+
+    // ---- tile loads: LDS-direct, each lane its own (swizzled) vector ----
+    const int kst = (int)a.ks[1] * ESZ, vst = (int)a.vs[1] * ESZ;
+    uint32_t koff[NL], voff[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        const int vi = ((SPLITK ? 0 : wave * NL) + i) * 64 + lane, r = vi / CH, s = vi - r * CH;
+        const int kc = s ^ TL::kswz(r), vc = s ^ TL::vswz(r);
+        koff[i] = kc * EPV < a.d ? (uint32_t)(r * kst + kc * 16) : OOB;
+        voff[i] = vc * EPV < a.d ? (uint32_t)(r * vst + vc * 16) : OOB;
+    }
+    const T* kbase = (const T*)a.k + n * a.ks[0] + hk * a.ks[2];
+    const T* vbase = (const T*)a.v + n * a.vs[0] + hk * a.vs[2];
+    const uint32_t lds0 = lds_address(lds) + (SPLITK ? wave * 2 * TL::STAGE : 0);
+    auto load_tile = [&](int k0, int stage) {
+        const uint32_t dst = lds0 + stage * TL::STAGE;
+        const int valid = min(kend - k0, BK);
+        const auto kr = make_rsrc(kbase + (int64_t)k0 * a.ks[1], (uint32_t)((valid - 1) * kst + a.d * ESZ));
+        const auto vr = make_rsrc(vbase + (int64_t)k0 * a.vs[1], (uint32_t)((valid - 1) * vst + a.d * ESZ));
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const uint32_t at = dst + ((SPLITK ? 0 : wave * NL) + i) * 1024;
+            dma16(kr, koff[i], __builtin_amdgcn_readfirstlane(at));
+            dma16(vr, voff[i], __builtin_amdgcn_readfirstlane(at + KB));
+        }
+        if constexpr (EXTRA)
+            if (a.slopes) {
+                const auto pr = make_rsrc(a.kpos + n * a.kps + (int64_t)k0 * a.A,
+                                          (uint32_t)(valid * a.A * 4));
+#pragma unroll
+                for (int x = 0; x < 3; ++x)
+                    if (x < a.A && (SPLITK || wave == x))
+                        dma4(pr, lane < BK ? (uint32_t)((lane * a.A + x) * 4) : OOB,
+                             __builtin_amdgcn_readfirstlane(dst + 2 * KB + x * 256));
+            }
+    };
+
+    accx16 o[QT][DT];
+    float M[QT], l[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        M[t] = -INFINITY;
+        l[t] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[t][d] = accx16{};
+    }
+    constexpr int KX = CH % 8 == 0 ? 4 : 2;    // vector pairs that the swizzle mixes
+    const int kswz = TL::kswz(col);
+    const uint32_t kread = (uint32_t)(col * RB + ((half ^ kswz) * 16));
+    // 16-bit V: this lane's row and column of a transposing read
+    const int vrow = 4 * half + (lane % 16) / 4;
+    const int vcol = 2 * ((lane / 16) % 2) + (lane % 4) / 2;
+
+    if (ntiles > 0) load_tile(kbeg, 0);
+    for (int it = 0; it < ntiles; ++it) {
+        const int k0 = kbeg + it * STEP;
+        const uint32_t src = lds0 + (it & 1) * TL::STAGE;
+        dma_wait<0>();
+        lds_read_drain();
+        if constexpr (!SPLITK) bare_barrier();
+        if (it + 1 < ntiles) load_tile(k0 + STEP, (it + 1) & 1);
+        if (k0 >= whi || k0 + BK <= wlo) continue;             // no row of this wave sees it
+        const bool whole = k0 >= wlo_max && k0 + BK <= whi_min; // every row sees all of it
+
+        // ---- scores ----
+        accx16 s[QT][KT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int k = 0; k < KT; ++k) s[t][k] = accx16{};
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int c = 0; c < CH / 2; ++c) {
+                const uint4 kf = lds_read16(
+                    src + (kread ^ ((c % KX) * 32)) + (c / KX) * (32 * KX) + k * 32 * RB);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) Mfma32<T>::step(kf, q[t][c], s[t][k]);
+            }
+        if constexpr (EXTRA) {
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    uint4 kp[3];
+                    if (a.slopes)
+#pragma unroll
+                        for (int x = 0; x < 3; ++x)
+                            if (x < a.A)
+                                kp[x] = lds_read16(src + 2 * KB + x * 256 +
+                                                   (32 * k + 8 * g + 4 * half) * 4);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t)
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            float v = s[t][k][4 * g + b] * p.pre;
+                            if (a.cap > 0.0f) {
+                                if constexpr (ESZ == 4) {
+                                    v = a.cap * tanhf(v / a.cap);
+                                } else {
+                                    // tanh x = 1 - 2 / (2^(2 x log2 e) + 1)
+                                    const float e = __builtin_amdgcn_exp2f(v * (2.8853900818f / a.cap));
+                                    v = a.cap - 2.0f * a.cap * __builtin_amdgcn_rcpf(e + 1.0f);
+                                }
+                            }
+                            if (a.slopes) {
+                                uint32_t dist = 0;
+#pragma unroll
+                                for (int x = 0; x < 3; ++x)
+                                    if (x < a.A)
+                                        dist = sad(qp[t][x],
+                                                   (b == 0 ? kp[x].x : b == 1 ? kp[x].y
+                                                    : b == 2 ? kp[x].z : kp[x].w) ^ 0x80000000u, dist);
+                                v -= slope[t] * (float)dist;
+                            }
+                            s[t][k][4 * g + b] = v;
+                        }
+                }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4;
+                        if (j < lo[t] || j >= hi[t]) s[t][k][i] = -INFINITY;
+                    }
+        }
+
+        // ---- running maximum and sum, weights ----
+        uint4 pf[QT][KT * 2];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            float mx = s[t][0][0];
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][k][i]);
+            mx = half_max(mx) * p.c;
+            // the maximum follows only when weights would pass 2^8: they stay
+            // within the 16-bit range and the sums within fp32
+            if (__any(mx > M[t] + 8.0f)) {
+                const float mn = fmaxf(M[t], mx);
+                const float alpha = M[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[t] - mn);
+                M[t] = mn;
+                l[t] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+            }
+            const float base = M[t] == -INFINITY ? 0.0f : M[t];
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k][i], p.c, -base));
+                    s[t][k][i] = w;
+                    sum += w;
+                }
+            l[t] += sum;
+            if constexpr (ESZ == 2)
+#pragma unroll
+                for (int k = 0; k < 2 * KT; ++k) {
+                    auto w = [&](int i) { return s[t][k / 2][8 * (k % 2) + i]; };
+                    // one rounding of the weights to the storage type: the matrix
+                    // instruction takes both operands in it
+                    pf[t][k] = make_uint4(pack2<T>(w(0), w(1)), pack2<T>(w(2), w(3)),
+                                          pack2<T>(w(4), w(5)), pack2<T>(w(6), w(7)));
+                }
+        }
+
+        // ---- values ----
+        // Keys that only some rows see may hold NaN or infinities, and 0 x NaN
+        // would reach the others: where a tile is not seen whole, non-finite
+        // values are looked for and then added key by key, to their rows alone.
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            if constexpr (ESZ == 2) {
+                uint4 vf[2 * KT];
+#pragma unroll
+                for (int k = 0; k < 2 * KT; ++k) {
+                    const int ch = (4 * d + vcol) ^ TL::vswz(vrow);
+                    const uint32_t at = src + KB + (16 * k + vrow) * RB + ch * 16 + (lane & 1) * 8;
+                    const uint2 x = lds_read_columns(at), y = lds_read_columns(at + 8 * RB);
+                    vf[k] = make_uint4(x.x, x.y, y.x, y.y);
+                }
+                bool clean = true;
+                if (!whole) {
+                    float z = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 2 * KT; ++k)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const uint32_t u = w == 0 ? vf[k].x : w == 1 ? vf[k].y : w == 2 ? vf[k].z : vf[k].w;
+                            T e[2];
+                            __builtin_memcpy(e, &u, 4);
+                            z += (float)e[0] * 0.0f + (float)e[1] * 0.0f;
+                        }
+                    clean = !__any(!(z == 0.0f));
+                }
+                if (clean) {
+#pragma unroll
+                    for (int k = 0; k < 2 * KT; ++k)
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) Mfma32<T>::step(vf[k], pf[t][k], o[t][d]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2 * KT; ++k)
+#pragma unroll 1
+                        for (int e = 0; e < 16; ++e) {
+                            const uint32_t m = half == e / 8 ? (e & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
+                            const int w = (e / 2) & 3;
+                            auto only = [&](const uint4& u) {
+                                return make_uint4(w == 0 ? u.x & m : 0u, w == 1 ? u.y & m : 0u,
+                                                  w == 2 ? u.z & m : 0u, w == 3 ? u.w & m : 0u);
+                            };
+                            const int j = k0 + 16 * k + 4 * (e / 8) + (e & 3) + 8 * ((e >> 2) & 1);
+                            const uint4 vk = only(vf[k]);
+#pragma unroll
+                            for (int t = 0; t < QT; ++t) {
+                                accx16 one = accx16{};
+                                Mfma32<T>::step(vk, only(pf[t][k]), one);
+                                const bool sees = j >= lo[t] && j < hi[t];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[t][d][i] += sees ? one[i] : 0.0f;
+                            }
+                        }
+                }
+            } else {
+                float vf[16 * KT];
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        vf[16 * k + i] = lds_read_f32(
+                            src + KB + (32 * k + 8 * (i / 4) + 4 * half + i % 4) * RB + (32 * d + col) * 4);
+                bool clean = true;
+                if (!whole) {
+                    float z = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 16 * KT; ++i) z += vf[i] * 0.0f;
+                    clean = !__any(!(z == 0.0f));
+                }
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (clean) {
+#pragma unroll
+                            for (int t = 0; t < QT; ++t)
+                                o[t][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[16 * k + i], s[t][k][i],
+                                                                               o[t][d], 0, 0, 0);
+                        } else {
+#pragma unroll 1
+                            for (int e = 0; e < 2; ++e) {
+                                const int j = k0 + 32 * k + 8 * (i / 4) + 4 * e + i % 4;
+#pragma unroll
+                                for (int t = 0; t < QT; ++t) {
+                                    const bool sees = j >= lo[t] && j < hi[t];
+                                    const accx16 one = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                                        half == e ? vf[16 * k + i] : 0.0f, half == e ? s[t][k][i] : 0.0f,
+                                        accx16{}, 0, 0, 0);
+#pragma unroll
+                                    for (int x = 0; x < 16; ++x) o[t][d][x] += sees ? one[x] : 0.0f;
+                                }
+                            }
+                        }
+                    }
+            }
+        }
+    }
+
+#pragma unroll
+    for (int t = 0; t < QT; ++t) l[t] += __shfl_xor(l[t], 32);
+    auto row_of = [&](int r, int& i, int& h) {
+        i = r / G;
+        h = hk * G + r - i * G;
+    };
+    // four consecutive elements of a row: normalised, or this split's part
+    auto store4 = [&](int r, int e, float w, float x0, float x1, float x2, float x3) {
+        if (p.splits > 1) {
+            float* part = p.part + (((int64_t)split * a.N * a.Hk + group) * p.rows + r) * a.d + e;
+            *(float4*)part = make_float4(x0, x1, x2, x3);
+            return;
+        }
+        int i, h;
+        row_of(r, i, h);
+        T* y = (T*)a.out + n * a.os[0] + i * a.os[1] + h * a.os[2] + e;
+        const float inv = w == 0.0f ? 0.0f : 1.0f / w;
+        Vec4<T>::store(y, make_float4(x0 * inv, x1 * inv, x2 * inv, x3 * inv));
+    };
+    auto store_ml = [&](int r, float m, float w) {
+        float* ml = p.ml + (((int64_t)split * a.N * a.Hk + group) * p.rows + r) * 2;
+        ml[0] = m;
+        ml[1] = w;
+    };
+    if constexpr (!SPLITK || NW == 1) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const int r = row0 + 32 * t + col;
+            if (r >= p.rows) continue;
+            if (p.splits > 1 && half == 0) store_ml(r, M[t], l[t]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int e = 32 * d + 8 * g + 4 * half;
+                    if (e < a.d)
+                        store4(r, e, l[t], o[t][d][4 * g], o[t][d][4 * g + 1], o[t][d][4 * g + 2],
+                               o[t][d][4 * g + 3]);
+                }
+        }
+    } else {
+        // the waves' parts meet in LDS, each brought to the common maximum
+        float* f = (float*)lds;
+        float* ml = f + NW * 32 * DP;
+        dma_wait<0>();
+        __syncthreads();
+        if (half == 0) {
+            ml[(wave * 32 + col) * 2] = M[0];
+            ml[(wave * 32 + col) * 2 + 1] = l[0];
+        }
+        __syncthreads();
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, ml[(w * 32 + col) * 2]);
+        const float scale = M[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[0] - m);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(float4*)&f[(wave * 32 + col) * DP + 32 * d + 8 * g + 4 * half] =
+                    make_float4(o[0][d][4 * g] * scale, o[0][d][4 * g + 1] * scale,
+                                o[0][d][4 * g + 2] * scale, o[0][d][4 * g + 3] * scale);
+        __syncthreads();
+        const int rows = min(32, p.rows - row0);
+        for (int x = threadIdx.x; x < rows * (DP / 4); x += NW * 64) {
+            const int rr = x / (DP / 4), e = 4 * (x % (DP / 4));
+            if (e >= a.d) continue;
+            float top = -INFINITY, w = 0.0f;
+            for (int v = 0; v < NW; ++v) top = fmaxf(top, ml[(v * 32 + rr) * 2]);
+            float4 sum = make_float4(0, 0, 0, 0);
+            for (int v = 0; v < NW; ++v) {
+                const float mv = ml[(v * 32 + rr) * 2];
+                w += mv == -INFINITY ? 0.0f : ml[(v * 32 + rr) * 2 + 1] * __builtin_amdgcn_exp2f(mv - top);
+                const float4 part = *(const float4*)&f[(v * 32 + rr) * DP + e];
+                sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
+            }
+            if (p.splits > 1 && e == 0) store_ml(row0 + rr, top, w);
+            store4(row0 + rr, e, w, sum.x, sum.y, sum.z, sum.w);
+        }
+    }
+}
+
+template <typename T, int DP>
+void launch_tile(const AttentionArgs& a, const AttentionPlan& p, const AttentionChoice& c, hipStream_t s)
+{
+    const dim3 grid((uint32_t)c.blocks);
+    const bool extra = a.cap > 0.0f || a.slopes;
+    if (c.splitk) {
+        constexpr int NT = 64 * AttentionTile<T, DP, 1, true>::NW;
+        if (extra) PPIPE_LAUNCH((attention_kernel<T, DP, 1, true, true>), grid, dim3(NT), 0, s, a, p);
+        else PPIPE_LAUNCH((attention_kernel<T, DP, 1, true, false>), grid, dim3(NT), 0, s, a, p);
+    } else {
+        if (extra) PPIPE_LAUNCH((attention_kernel<T, DP, 1, false, true>), grid, dim3(256), 0, s, a, p);
+        else PPIPE_LAUNCH((attention_kernel<T, DP, 1, false, false>), grid, dim3(256), 0, s, a, p);
+    }
+}
+
+template <typename T>
+void launch_type(const AttentionArgs& a, const AttentionPlan& p, const AttentionChoice& c, hipStream_t s)
+{
+    if (a.d <= 32) launch_tile<T, 32>(a, p, c, s);
+    else if (a.d <= 64) launch_tile<T, 64>(a, p, c, s);
+    else if (a.d <= 96) launch_tile<T, 96>(a, p, c, s);
+    else if (a.d <= 128) launch_tile<T, 128>(a, p, c, s);
+    else if (a.d <= 192) launch_tile<T, 192>(a, p, c, s);
+    else launch_tile<T, 256>(a, p, c, s);
+}
+
+}  // namespace ppipe

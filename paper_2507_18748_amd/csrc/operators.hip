@@ -171,8 +171,7 @@ int ppipe::check_attention(const ppipe_attention_desc& t, const std::string& who
     if (t.axes < 0 || t.axes > 3) return bad(who + "positions have one to three axes");
     if (t.spans_stride % 2) return bad(who + "spans stride must be even");
     if (t.heads > MAX_HEADS || t.kv_len > ATTENTION_MAX_LEN || t.q_len > ATTENTION_MAX_LEN ||
-        (int64_t)t.q_len * t.heads > 0x7fffffff ||
-        (int64_t)t.batch * t.q_len * t.heads > ((int64_t)1 << 34))
+        (t.q_len && t.heads && t.batch > 0x7fffffff / ((int64_t)t.q_len * t.heads)))
         return unsupported(who + "attention of this size is not supported");
     const int esz = dtype_size(t.dtype);
     const int64_t nq[3] = {t.batch, t.q_len, t.heads}, nk[3] = {t.batch, t.kv_len, t.kv_heads};
