@@ -125,6 +125,12 @@ size_t attention_workspace(int dt, const AttentionArgs& a, int cus)
     return c.splits > 1 ? (size_t)c.splits * a.N * a.Lq * a.H * (a.d + 2) * 4 : 0;
 }
 
+bool attention_fits(int dt, const AttentionArgs& a, int cus)
+{
+    const AttentionChoice c = choose(dt, a, cus);
+    return c.blocks < 1 << 24 && (c.splits == 1 || (double)a.N * a.Lq * a.H * (a.d / 4) < 4294967040.0);
+}
+
 int attention_launches(int dt, const AttentionArgs& a, int cus)
 {
     return choose(dt, a, cus).splits > 1 ? 2 : 1;

@@ -313,6 +313,8 @@ hipError_t launch_group_norm(int dt, const GroupNormArgs& a, void* ws, int cus, 
                              hipStream_t s);
 const char* group_norm_name(int dt, int N, int P, int C, int G, int cus, int launch);
 int group_norm_launches(int dt, int N, int P, int C, int G, int cus);
+// whether the launches fit a grid (2^32 - 1 threads)
+bool group_norm_fits(int dt, int N, int P, int C, int G, int cus);
 
 // Rotary positions: x, y [N][L][H][d] by strides (batch, token, head).
 struct RotaryArgs {
@@ -325,7 +327,7 @@ struct RotaryArgs {
     double base;
     int64_t xs[3], ys[3], ps;
 };
-hipError_t launch_rotary(int dt, const RotaryArgs& a, hipStream_t s);
+hipError_t launch_rotary(int dt, const RotaryArgs& a, int cus, hipStream_t s);
 const char* rotary_name(int dt);
 
 // Spans of visible keys (ppipe_attention_spans).
@@ -352,6 +354,7 @@ size_t attention_workspace(int dt, const AttentionArgs& a, int cus);
 hipError_t launch_attention(int dt, const AttentionArgs& a, void* ws, int cus, int launch,
                             hipStream_t s);
 int attention_launches(int dt, const AttentionArgs& a, int cus);
+bool attention_fits(int dt, const AttentionArgs& a, int cus);
 const char* attention_name(int dt, const AttentionArgs& a, int cus, int launch);
 
 // n elements of x (in_dt) converted to y (out_dt); narrowing rounds to

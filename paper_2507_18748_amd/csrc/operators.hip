@@ -45,8 +45,9 @@ int ppipe::check_group_norm(int dt, int64_t batch, int64_t pixels, int C, int G,
     if (C % epv || C > GROUP_NORM_MAX_C)
         return unsupported(who + "group norm needs channels % " + std::to_string(epv) +
                            " == 0, at most " + std::to_string(GROUP_NORM_MAX_C));
-    if (batch * pixels > 0x7fffffff)
-        return unsupported(who + "more than 2^31 - 1 pixels");
+    if (batch * pixels > 0x7fffffff ||
+        (batch && pixels && !group_norm_fits(dt, (int)batch, (int)pixels, C, G, device_cus())))
+        return unsupported(who + "group norm of this many images or pixels is not supported");
     return PPIPE_OK;
 }
 
@@ -125,8 +126,8 @@ int ppipe::check_rotary(const ppipe_rotary_desc& r, const std::string& who)
         return bad(who + "rotary pairs must be one to head_dim / 2 in all");
     if ((r.shared | r.adjacent) & ~1) return bad(who + "shared and adjacent are 0 or 1");
     if (!(r.base > 0.0) || std::isinf(r.base)) return bad(who + "rotary base must be positive");
-    if ((int64_t)r.batch * r.tokens > 0x7fffffff)
-        return unsupported(who + "more than 2^31 - 1 tokens");
+    if ((int64_t)r.batch * r.tokens >= 1 << 24)       // a block each at most, 256 threads
+        return unsupported(who + "2^24 tokens and more");
     if (r.heads > MAX_HEADS) return unsupported(who + "more than 65536 heads");
     const int64_t n[3] = {r.batch, r.tokens, r.heads};
     int rc = check_batch_stride(r.positions_stride, r.batch, who);
@@ -184,6 +185,10 @@ int ppipe::check_attention(const ppipe_attention_desc& t, const std::string& who
     if (rc == PPIPE_OK) rc = check_strides("out", t.out_strides, nq, esz);
     if (rc != PPIPE_OK) return rc;
     if (overlaps_itself(t.out_strides, nq, t.head_dim)) return bad(who + "out overlaps itself");
+    if (t.batch && t.q_len &&
+        !attention_fits(t.dtype, attention_args(t, nullptr, nullptr, nullptr, nullptr, nullptr,
+                                                nullptr, nullptr, nullptr), device_cus()))
+        return unsupported(who + "attention of this size is not supported");
     return PPIPE_OK;
 }
 
@@ -256,7 +261,7 @@ int ppipe_rotary(const ppipe_rotary_desc* desc, const void* x, const int32_t* po
     }
     return launched("rotary launch",
                     launch_rotary(desc->dtype, rotary_args(*desc, x, positions, y),
-                                  (hipStream_t)stream));
+                                  device_cus(), (hipStream_t)stream));
 }
 
 int ppipe_attention_spans(int32_t* spans, int32_t batch, int32_t q_len, int32_t kv_len,

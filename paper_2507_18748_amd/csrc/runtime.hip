@@ -880,7 +880,7 @@ hipError_t enqueue_layer(const ppipe_partition* P, const LayerRT& l, int batch, 
                 e = launch_group_norm(P->dtype, norm_args(l, batch, x, y), W.ws, P->cus, i, s);
             else if (rot && i == 0)
                 e = launch_rotary(P->dtype, rotary_args(rotary_desc(l, P->dtype, batch), x, l.pos,
-                                                        W.ws), s);
+                                                        W.ws), P->cus, s);
             else
                 e = launch_attention(P->dtype, layer_attention(l, P->dtype, batch, x, y, W.ws),
                                      (uint8_t*)W.ws + rotated_bytes(l, P->dtype, batch), P->cus,

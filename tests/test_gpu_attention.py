@@ -325,6 +325,20 @@ def test_beyond_32_bit_offsets():
     del big, k, v
 
 
+def test_workspace_too_small_is_refused():
+    q, k, v = tensors("f16", 1, 1, 30000, 8, 1, 128)
+    out = torch.empty_like(q)
+    st = [t.stride()[:3] for t in (q, k, v, out)]
+    need = attention_workspace(attention_desc("f16", 1, 1, 30000, 8, 1, 128, *st, 0.1))
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for ptr, size in ((0, need), (ws.data_ptr(), need - 1), (ws.data_ptr() + 4, need)):
+        with pytest.raises(PpipeError) as e:
+            attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), "f16", 1, 1, 30000,
+                      8, 1, 128, *st, 0.1, workspace_ptr=ptr, workspace_bytes=size)
+        assert e.value.status == -1
+
+
 @pytest.mark.parametrize("lq,lk", [(200, 200), (1, 5000)])
 def test_captured_on_another_stream_and_repeatable(lq, lk):
     q, k, v = tensors("bf16", 2, lq, lk, 4, 2, 64)

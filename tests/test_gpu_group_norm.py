@@ -121,6 +121,18 @@ def test_large_activations():
         R.check(run(x, 8, gamma, None, act=act, dtype="f32"), ref, bound, "f32")
 
 
+def test_workspace_too_small_is_refused():
+    n, p, c, g = 2, 50000, 64, 8
+    need = group_norm_workspace("f16", n, p, c, g)
+    assert need > 0
+    x = torch.zeros(n, p, c, dtype=torch.float16, device="cuda")
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for ptr, size in ((0, need), (ws.data_ptr(), need - 1)):
+        with pytest.raises(PpipeError) as e:
+            group_norm(x.data_ptr(), x.data_ptr(), "f16", n, p, c, g, 0, 0, 1e-5, "none", ptr, size)
+        assert e.value.status == -1
+
+
 @pytest.mark.parametrize("p", [196, 30000])
 def test_captured_on_another_stream_and_repeatable(p):
     """Two graphs with workspaces of their own, replayed in turn and together with
