@@ -6,8 +6,10 @@
 // each image's group.  Bound by memory: the least is one read and one write.
 //
 // A block holds a slab (pixels x whole groups of one image) in registers, at
-// most 256 KB, and takes its mean and then the squared differences from it
-// from there (no cancellation, fp32 throughout).  Where a slab is all pixels
+// most 256 KB (32 vectors of 16 bytes for each of 512 threads).  Each thread
+// takes the mean and the squared differences of its own values, and these are
+// joined by the parallel form for sums of squares (Chan, Golub, LeVeque), fp32
+// throughout.  Where a slab is all pixels
 // it writes the outputs at once: one read, one write, one launch.  Larger maps
 // take two launches: slabs leave their mean and sum of squared differences,
 // the second launch joins those (Chan's formula) and reads the map again.
@@ -18,19 +20,50 @@
 namespace ppipe {
 namespace {
 
-__device__ __forceinline__ float norm_act(float z, int act)
+template <int act> __device__ __forceinline__ float norm_act(float z)
 {
-    if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;      // a NaN stays one
-    if (act == ACT_RELU6) return z < 0.0f ? 0.0f : z > 6.0f ? 6.0f : z;
+    // (maximum and minimum that keep a NaN)
+    if (act == ACT_RELU) return __builtin_elementwise_maximum(z, 0.0f);
+    if (act == ACT_RELU6) return __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, 0.0f), 6.0f);
     if (act == ACT_SILU)
         return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
-    if (act == ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    if (act == ACT_GELU) {
+        // Phi(-|z|) = erfc(|z| / sqrt 2) / 2 by Abramowitz and Stegun 7.1.26, off by
+        // at most 7.5e-8 (half of its 1.5e-7)
+        const float x = fabsf(z) * 0.70710678f;
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
+        float q = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+        q = __builtin_fmaf(q, t, 1.421413741f);
+        q = __builtin_fmaf(q, t, -0.284496736f);
+        q = __builtin_fmaf(q, t, 0.254829592f);
+        const float h = 0.5f * q * t * __builtin_amdgcn_exp2f(-1.4426950408889634f * x * x);
+        return z * (z < 0.0f ? h : 1.0f - h);
+    }
     return z;
+}
+
+// f(integral_constant) of the activation: one branch for all elements.
+template <typename F> __device__ __forceinline__ void with_act(int act, F&& f)
+{
+    if (act == ACT_NONE) f(std::integral_constant<int, ACT_NONE>{});
+    else if (act == ACT_RELU) f(std::integral_constant<int, ACT_RELU>{});
+    else if (act == ACT_RELU6) f(std::integral_constant<int, ACT_RELU6>{});
+    else if (act == ACT_SILU) f(std::integral_constant<int, ACT_SILU>{});
+    else f(std::integral_constant<int, ACT_GELU>{});
 }
 
 template <typename T, int V>
 __device__ __forceinline__ void unpack(const uint4& u, float* f)
 {
+    if constexpr (std::is_same<T, __bf16>::value) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+        return;
+    }
     T e[V];
     __builtin_memcpy(e, &u, 16);
 #pragma unroll
@@ -49,7 +82,8 @@ __device__ __forceinline__ uint4 pack(const float* f)
 
 // How a call is cut.
 struct NormPlan {
-    bool single;       // a block takes one group (its vectors may begin and end inside it)
+    bool single;       // a block takes one group
+    bool whole;        // of whole vectors
     int cv;            // vectors of a pixel that a block takes
     int groups;        // groups of a block
     int chunks;        // blocks per image and slab
@@ -58,56 +92,91 @@ struct NormPlan {
     FastDiv div_cv;
 };
 
-constexpr int NORM_R = 16, NORM_NT = 1024;
+constexpr int NORM_R = 32, NORM_SLAB_R = 8, NORM_NT = 512;
 
+enum NormMode {
+    MIXED = 0,         // several groups of a pixel, vectors of several groups
+    SEVERAL = 1,       // several groups of whole vectors
+    ONE = 2,           // one group of whole vectors, a row no longer than the block
+    ANY = 3            // one group whose rows begin or end inside a vector, or are longer
+};
+
+// One launch or two.  A block alone takes about 4 us and 0.45 us for each vector
+// that a thread holds (fp32: 0.3), and blocks beyond one per CU come in turn; two
+// launches take about 9 us and three passes at 5 TB/s.  Measured both ways (one /
+// two, us): 64 x 56x56x256 bf16 55 / 67, 8 x the same 14.8 / 17.6, 2 x 9.9 / 11.6,
+// 64 x 14x14x1024 15.6 / 25, 32 x 40x40x96 17.8 / 21.6, 1 x 112x112x64 in 32
+// groups 29.5 / 16.4.  Rows read in pieces of 256 or 1024 bytes where slabs fill
+// the chip anyway: 1 x 128x128x320 f16 23 -> 24 and 33 (64 bytes stay).
 NormPlan norm_plan(int dt, int N, int P, int C, int G, int cus)
 {
     const int esz = dtype_size(dt), V = 16 / esz, cpg = C / G;
-    NormPlan p;
+    auto pixels = [&](const NormPlan& p, int nt, int r) {    // of a slab, below 2 GiB apart
+        const int64_t n = p.cv <= nt ? (int64_t)(nt / p.cv) * r
+                          : nt == NORM_NT ? r / ((p.cv + nt - 1) / nt) : 0;
+        return std::min<int64_t>(n, 0x7fffffff / ((int64_t)C * esz));
+    };
     // Rows of a group from 64 bytes on are read well by themselves.  Smaller
     // groups are taken several to a block: the least number whose channels are
     // whole vectors, then up to 64 bytes while the grid still fills the chip.
-    p.single = cpg * esz >= 64;
-    if (p.single) {
-        p.cv = cpg % V ? cpg / V + 2 : cpg / V;
-        p.groups = 1;
-        p.chunks = G;
-    } else {
-        int l = cpg;
-        while (l % V) l += cpg;                       // least common multiple
-        const int all = C / l;
-        int m = 1;
-        for (int q = 2; q <= all && q * l * esz <= 64; ++q)
-            if (all % q == 0 && (int64_t)N * (all / q) >= cus) m = q;
-        p.cv = m * l / V;
-        p.groups = m * l / cpg;
-        p.chunks = all / m;
-    }
-    // pixels of a slab: what the largest block holds, below 2 GiB apart
-    auto pixels = [&](int nt, int r) {
-        const int64_t n = p.single ? (int64_t)nt * r / p.cv : (int64_t)(nt / p.cv) * r;
-        return std::min<int64_t>(n, 0x7fffffff / ((int64_t)C * esz));
+    auto cut = [&](int fill) {
+        NormPlan p;
+        p.single = cpg * esz >= 64;
+        p.whole = cpg % V == 0;
+        if (p.single) {
+            p.cv = p.whole ? cpg / V : cpg / V + 2;
+            p.groups = 1;
+            p.chunks = G;
+        } else {
+            int l = cpg;
+            while (l % V) l += cpg;                       // least common multiple
+            const int all = C / l;
+            int m = 1;
+            for (int q = 2; q <= all && q * l * esz <= 64; ++q)
+                if (all % q == 0 && (int64_t)N * (all / q) >= fill) m = q;
+            p.cv = m * l / V;
+            p.groups = m * l / cpg;
+            p.chunks = all / m;
+        }
+        p.div_cv = fast_div_of((uint32_t)p.cv);
+        return p;
     };
+    NormPlan p = cut(cus);
     p.nt = 256;
-    for (p.r = 1; p.r < 4 && pixels(256, p.r) < P; p.r *= 2) {}
-    if (pixels(p.nt, p.r) < P) {
+    for (p.r = 1; p.r < 4 && pixels(p, 256, p.r) < P; p.r *= 2) {}
+    if (pixels(p, p.nt, p.r) < P) {
         p.nt = NORM_NT;
-        for (p.r = 2; p.r < NORM_R && pixels(p.nt, p.r) < P; p.r *= 2) {}
+        const int most = p.single && !(p.whole && p.cv <= NORM_NT) ? NORM_R / 2 : NORM_R;
+        for (p.r = 4; p.r < most && pixels(p, p.nt, p.r) < P; p.r *= 2) {}
     }
-    p.px = (int)std::min<int64_t>(P, pixels(p.nt, p.r));
-    p.slabs = p.px < 1 ? 0 : (P + p.px - 1) / p.px;
-    if (p.slabs > 1) p.px = (P + p.slabs - 1) / p.slabs;
-    p.div_cv = fast_div_of((uint32_t)p.cv);
+    const double rounds = (double)(((int64_t)N * p.chunks + cus - 1) / cus);
+    const double one = 4.0 + (esz == 2 ? 0.45 : 0.3) * ((double)P * p.cv / p.nt) * rounds;
+    const double two = 9.0 + 3.0 * N * (double)P * C * esz / 5e6;
+    p.px = P;
+    p.slabs = 1;
+    if (pixels(p, p.nt, p.r) >= P && one <= two) return p;
+    p = cut(0);
+    p.nt = NORM_NT;
+    p.r = NORM_SLAB_R;
+    while (p.r > 4 && pixels(p, p.nt, p.r / 2) > 0 &&
+           (int64_t)N * p.chunks * ((P + pixels(p, p.nt, p.r) - 1) / pixels(p, p.nt, p.r)) < 4 * cus)
+        p.r /= 2;
+    while (pixels(p, p.nt, p.r) < 1) p.r *= 2;
+    p.px = (int)std::min<int64_t>(P, pixels(p, p.nt, p.r));
+    p.slabs = (P + p.px - 1) / p.px;
+    p.px = (P + p.slabs - 1) / p.slabs;
     return p;
 }
 
-template <typename T, int NT, int R, bool SINGLE>
-__global__ void __launch_bounds__(NT)
+template <typename T, int NT, int R, int MODE>
+__global__ void __launch_bounds__(NT, NT != NORM_NT ? 1 : R < NORM_R && (MODE == SEVERAL || MODE == ONE) ? 4 : 2)
 group_norm_kernel(GroupNormArgs a, NormPlan p, float* part)
 {
     constexpr int ESZ = (int)sizeof(T), V = 16 / ESZ, NW = NT / 64;
-    __shared__ float red[SINGLE ? NW : NT * V];
-    __shared__ float stat[SINGLE ? 1 : 64];
+    constexpr bool SINGLE = MODE >= ONE;
+    constexpr int S = MODE == MIXED ? V : 1;       // statistics of a thread's channels
+    __shared__ float2 red[SINGLE ? 1 : NT * S];
+    __shared__ float4 stat[64];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     // blocks of one image side by side on one XCD: their rows share cache lines
     const uint32_t per = gridDim.x / NUM_XCD, rem = gridDim.x % NUM_XCD, xcd = blockIdx.x % NUM_XCD;
@@ -123,72 +192,128 @@ group_norm_kernel(GroupNormArgs a, NormPlan p, float* part)
     const auto rx = make_rsrc(x, (uint32_t)px * (uint32_t)(a.C * ESZ));
 
     // ---- the slab into registers ----
+    // Vector i of a thread lies in row slot + i slots of the slab, always in one
+    // column; where rows are longer than the block: row i / per_row, column col +
+    // (i % per_row) NT.
     uint4 u[R];
-    uint32_t off[R];
-    const int cvs = SINGLE ? min(p.cv, (c0 + cpg - 1) / V - v0 + 1) : p.cv;
-    const int slots = SINGLE ? 1 : NT / p.cv, slot = SINGLE ? 0 : fast_div(tid, p.div_cv);
-    const int col = SINGLE ? 0 : tid - slot * p.cv;
+    const int cvs = SINGLE ? (c0 + cpg - 1) / V - v0 + 1 : p.cv;
+    const int per_row = MODE == ANY ? (p.cv + NT - 1) / NT : 1;
+    const bool wide = MODE == ANY && per_row > 1;
+    const int slots = wide ? 1 : NT / p.cv;
+    const int slot = wide ? 0 : fast_div(tid, p.div_cv);
+    const int col = tid - slot * p.cv;
+    const uint32_t row_bytes = (uint32_t)(a.C * ESZ), step = (uint32_t)slots * row_bytes;
+    uint32_t off0 = (uint32_t)slot * row_bytes + (uint32_t)(v0 + col) * 16u;
+    // first vector of the thread outside the slab
+    int mine = wide || slot >= slots || col >= cvs ? 0 : (px - slot + slots - 1) / slots;
+    auto offset = [&](int i) {
+        if (wide) {
+            const int row = i / per_row, c = (i - row * per_row) * NT;
+            return row < px && col + c < cvs ? off0 + (uint32_t)row * row_bytes + (uint32_t)c * 16u : OOB;
+        }
+        return i < mine ? off0 + (uint32_t)i * step : OOB;
+    };
+#pragma unroll
+    for (int i = 0; i < R; ++i) u[i] = buf_load16(rx, offset(i));
+    // scale and shift of the thread's channels, on their way before they are needed
+    float ga[V], be[V];
+    auto affine = [&](int i) {
+        const int c = (v0 + col + (wide ? (i % per_row) * NT : 0)) * V;
+        const bool ok = p.slabs == 1 && offset(i) != OOB;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            ga[e] = ok && a.gamma ? a.gamma[c + e] : 1.0f;
+            be[e] = ok && a.beta ? a.beta[c + e] : 0.0f;
+        }
+    };
+    affine(0);
+    // which channels of vector i belong to the group (SINGLE: the first and
+    // last vector of a row may reach beyond it)
+    const bool ends = MODE == ANY && cpg % V != 0;
+    auto inside = [&](int i, int e) {
+        const int c = (v0 + col + (wide ? (i % per_row) * NT : 0)) * V + e;
+        return c >= c0 && c < c0 + cpg;
+    };
+
+    // ---- statistics of the thread's values, of one group or of each channel's ----
+    // Mean and squared differences of a thread's values x by sums of x - k and
+    // (x - k)^2, k its first value: a value far off the others counts in the sum of
+    // squares itself, so what cancels stays below (values of the thread) 2^-24 of it.
+    float k[S], sum[S], sq[S], cnt = 0.0f;
+#pragma unroll
+    for (int e = 0; e < S; ++e) sum[e] = sq[e] = 0.0f;
+    {
+        float v[V];
+        unpack<T, V>(u[0], v);
+#pragma unroll
+        for (int e = 0; e < S; ++e) k[e] = v[e];
+        if constexpr (MODE == ANY)
+#pragma unroll
+            for (int e = V - 1; e >= 0; --e)
+                if (inside(0, e)) k[0] = v[e];
+    }
+    // Each pass unpacks a vector and computes its offset when it comes to it: the
+    // compiler would do so for all at once, which does not fit the registers.
+    auto turn_to = [&](int i) {
+        asm volatile("" : "+v"(u[i].x), "+v"(u[i].y), "+v"(u[i].z), "+v"(u[i].w), "+v"(off0), "+v"(mine));
+        __builtin_amdgcn_sched_barrier(0);
+    };
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        int q, v;
-        bool ok;
-        if constexpr (SINGLE) {
-            const int idx = tid + NT * i;
-            q = fast_div(idx, p.div_cv);
-            v = idx - q * p.cv;
-            ok = q < px && v < cvs;
-        } else {
-            q = slot + i * slots;
-            v = col;
-            ok = slot < slots && q < px;
+        turn_to(i);
+        if (offset(i) == OOB) continue;
+        float v[V];
+        unpack<T, V>(u[i], v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const bool in = MODE != ANY || inside(i, e);
+            const float d = in ? v[e] - k[e % S] : 0.0f;
+            sum[e % S] += d;
+            sq[e % S] = __builtin_fmaf(d, d, sq[e % S]);
+            if constexpr (MODE == ANY) cnt += in ? 1.0f : 0.0f;
         }
-        off[i] = ok ? (uint32_t)q * (uint32_t)(a.C * ESZ) + (uint32_t)(v0 + v) * 16u : OOB;
-        u[i] = buf_load16(rx, off[i]);
     }
-    // which channels of vector i belong to the group (SINGLE: ends may not)
-    auto inside = [&](int i, int e) {
-        if constexpr (!SINGLE) return off[i] != OOB;
-        const int c = (int)(off[i] % (uint32_t)(a.C * ESZ)) / ESZ + e;
-        return off[i] != OOB && c >= c0 && c < c0 + cpg;
-    };
-    const bool ends = SINGLE && cpg % V != 0;
+    if constexpr (MODE != ANY) cnt = (float)(mine * (V / S));
+    const float inv = cnt > 0.0f ? 1.0f / cnt : 0.0f;
+    float mean[S], m2[S];
+#pragma unroll
+    for (int e = 0; e < S; ++e) {
+        const float m = sum[e] * inv, s = __builtin_fmaf(-sum[e], m, sq[e]);
+        mean[e] = cnt > 0.0f ? k[e] + m : 0.0f;
+        m2[e] = s < 0.0f ? 0.0f : s;
+    }
 
-    // ---- group sums of V values a thread, or of one where a vector lies in one group ----
-    const bool whole = cpg % V == 0;
-    auto reduce = [&](const float* f, float* out) {
-        if constexpr (SINGLE) {
-            float s = 0.0f;
+    // ---- of the groups: first the means are added, then the differences from the sum ----
+    auto wave_sum = [](float v) {
+        for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+        return v;
+    };
+    // partial (count, mean, squared differences) of a wave's part of a group
+    int parts, mygroup = 0;
+    if constexpr (SINGLE) {
+        const float n = wave_sum(cnt), m = n > 0.0f ? wave_sum(cnt * mean[0]) / n : wave_sum(0.0f);
+        const float d = mean[0] - m, s = wave_sum(cnt > 0.0f ? m2[0] + cnt * d * d : 0.0f);
+        if (lane == 0) stat[wave] = make_float4(n, m, s, 0.0f);
+        parts = NW;
+        __syncthreads();
+    } else {
+        if (slot < slots)
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += f[e];
-            for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m);
-            __syncthreads();
-            if (lane == 0) red[wave] = s;
-            __syncthreads();
-            s = 0.0f;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) s += red[w];
-            *out = s;
-        } else {
-            __syncthreads();
-            const int vp = whole ? 1 : V, width = p.cv * vp, each = whole ? cpg / V : cpg;
-            if (slot < slots) {
-                if (whole) {
-                    float s = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) s += f[e];
-                    red[tid] = s;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) red[tid * V + e] = f[e];
-                }
-            }
-            __syncthreads();
-            for (int g = wave; g < p.groups; g += NW) {
-                float s = 0.0f;
-                int q = lane / each, e = lane - q * each;
+            for (int e = 0; e < S; ++e) red[tid * S + e] = make_float2(mean[e], m2[e]);
+        __syncthreads();
+        const int width = p.cv * S, each = S == 1 ? cpg / V : cpg;
+        parts = max(NW / p.groups, 1);
+        const int full = px / slots, more = px - full * slots;   // pixels of a slot
+        for (int w = wave; w < p.groups * parts; w += NW) {
+            const int part = w / p.groups, g = w - part * p.groups;
+            const int q0 = slots * part / parts, q1 = slots * (part + 1) / parts;
+            auto walk = [&](auto&& f) {
+                int q = q0 + lane / each, e = lane % each;
                 const int dq = 64 / each, de = 64 - dq * each;
-                while (q < slots) {
-                    s += red[q * width + g * each + e];
+                float s = 0.0f;
+                while (q < q1) {
+                    const float2 v = red[q * width + g * each + e];
+                    s += f((float)(full + (q < more ? 1 : 0)), v);
                     q += dq;
                     e += de;
                     if (e >= each) {
@@ -196,43 +321,39 @@ group_norm_kernel(GroupNormArgs a, NormPlan p, float* part)
                         ++q;
                     }
                 }
-                for (int m = 32; m; m >>= 1) s += __shfl_xor(s, m);
-                if (lane == 0) stat[g] = s;
-            }
-            __syncthreads();
-            // of the thread's channels
-#pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = stat[min((col * V + e) / cpg, p.groups - 1)];
+                return wave_sum(s);
+            };
+            const int rows = max(0, min(q1, more) - min(q0, more)) + full * (q1 - q0);
+            const float n = (float)(rows * each);
+            const float m = n > 0.0f ? walk([](float c, float2 v) { return c * v.x; }) / n : 0.0f;
+            const float s = walk([m](float c, float2 v) {
+                const float d = v.x - m;
+                return v.y + c * (V / S) * d * d;      // a pixel of a thread: V / S values
+            });
+            if (lane == 0) stat[part * p.groups + g] = make_float4(n * (V / S), m, s, 0.0f);
         }
-    };
-    constexpr int S = SINGLE ? 1 : V;
+        __syncthreads();
+    }
+    // the parts join; S > 1: of each channel's group
+#pragma unroll
+    for (int e = 0; e < S; ++e) {
+        if constexpr (!SINGLE) mygroup = min((col * V + e) / cpg, p.groups - 1);
+        const int stride = SINGLE ? 1 : p.groups;
+        float m = 0.0f, n = 0.0f, s = 0.0f;
+        for (int q = 0; q < parts; ++q) {
+            const float4 v = stat[q * stride + mygroup];
+            m += v.x * v.y;
+            n += v.x;
+        }
+        m /= n;
+        for (int q = 0; q < parts; ++q) {
+            const float4 v = stat[q * stride + mygroup];
+            s += v.z + v.x * (v.y - m) * (v.y - m);
+        }
+        mean[e] = m;
+        m2[e] = s;
+    }
     const float count = (float)px * (float)cpg;
-    float f[V], mean[S], m2[S];
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        float v[V];
-        unpack<T, V>(u[i], v);
-#pragma unroll
-        for (int e = 0; e < V; ++e) f[e] += !ends || inside(i, e) ? v[e] : 0.0f;
-    }
-    reduce(f, mean);
-#pragma unroll
-    for (int e = 0; e < S; ++e) mean[e] /= count;
-#pragma unroll
-    for (int e = 0; e < V; ++e) f[e] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        float v[V];
-        unpack<T, V>(u[i], v);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float d = v[e] - mean[SINGLE ? 0 : e];
-            f[e] += (ends ? inside(i, e) : off[i] != OOB) ? d * d : 0.0f;
-        }
-    }
-    reduce(f, m2);
 
     if (p.slabs > 1) {
         // mean and sum of squared differences of this slab's groups
@@ -244,7 +365,7 @@ group_norm_kernel(GroupNormArgs a, NormPlan p, float* part)
             }
         } else if (slot == 0) {
 #pragma unroll
-            for (int e = 0; e < V; ++e)
+            for (int e = 0; e < S; ++e)
                 if ((col * V + e) % cpg == 0) {
                     out[(col * V + e) / cpg * 2] = mean[e];
                     out[(col * V + e) / cpg * 2 + 1] = m2[e];
@@ -253,43 +374,45 @@ group_norm_kernel(GroupNormArgs a, NormPlan p, float* part)
         return;
     }
     // ---- outputs ----
-    float rstd[S], ga[V], be[V];
+    float rstd[S];
 #pragma unroll
     for (int e = 0; e < S; ++e) rstd[e] = 1.0f / sqrtf(m2[e] / count + a.eps);
-    if constexpr (!SINGLE) {
+    // 16-bit: the mean goes into the shift (its rounding, 2^-24 of mean / deviation,
+    // is far below the output's); fp32 subtracts it first
+    auto finish_affine = [&] {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const int c = c0 + col * V + e;
-            ga[e] = (a.gamma ? a.gamma[c] : 1.0f) * rstd[e];
-            be[e] = a.beta ? a.beta[c] : 0.0f;
+            ga[e] *= rstd[e % S];
+            if constexpr (ESZ == 2) be[e] = __builtin_fmaf(-mean[e % S], ga[e], be[e]);
         }
-    }
+    };
+    finish_affine();
+    with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        if (off[i] == OOB) continue;
-        float v[V];
-        unpack<T, V>(u[i], v);
-        if constexpr (SINGLE) {
-            const int c = (int)(off[i] % (uint32_t)(a.C * ESZ)) / ESZ;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int cc = min(c + e, a.C - 1);
-                ga[e] = (a.gamma ? a.gamma[cc] : 1.0f) * rstd[0];
-                be[e] = a.beta ? a.beta[cc] : 0.0f;
+        for (int i = 0; i < R; ++i) {
+            turn_to(i);
+            const uint32_t off = offset(i);
+            if (off == OOB) continue;
+            if (wide && i > 0) {
+                affine(i);
+                finish_affine();
             }
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            v[e] = norm_act(__builtin_fmaf(v[e] - mean[SINGLE ? 0 : e], ga[e], be[e]), a.act);
-        T* dst = (T*)((uint8_t*)y + off[i]);
-        if (!ends || (inside(i, 0) && inside(i, V - 1))) {
-            *(uint4*)dst = pack<T, V>(v);
-        } else {
+            float v[V];
+            unpack<T, V>(u[i], v);
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                if (inside(i, e)) dst[e] = (T)v[e];
+                v[e] = norm_act<decltype(act)::value>(
+                    __builtin_fmaf(ESZ == 2 ? v[e] : v[e] - mean[e % S], ga[e], be[e]));
+            T* dst = (T*)((uint8_t*)y + off);
+            if (!ends || (inside(i, 0) && inside(i, V - 1))) {
+                *(uint4*)dst = pack<T, V>(v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (inside(i, e)) dst[e] = (T)v[e];
+            }
         }
-    }
+    });
 }
 
 // Second launch: a block joins the slabs' statistics of the groups that its
@@ -310,60 +433,89 @@ group_norm_apply_kernel(GroupNormArgs a, NormPlan p, const float* part, int cols
     const int rt = (int)(lin % (uint32_t)row_tiles), n = (int)(lin / (uint32_t)row_tiles);
     const int cpg = a.C / a.G, CV = a.C / V;
     const int nc = min(cols, CV - ct * cols);                // columns of this block
-    const int g0 = ct * cols * V / cpg, g1 = (ct * cols * V + nc * V - 1) / cpg;
-    for (int g = g0 + tid; g <= g1; g += APPLY_NT) {
-        const float* q = part + ((int64_t)n * p.slabs * a.G + g) * 2;
-        float mean = 0.0f, m2 = 0.0f;
-        for (int s = 0; s < p.slabs; ++s)
-            mean += q[(int64_t)s * a.G * 2] * ((float)min(p.px, a.P - s * p.px) / (float)a.P);
-        for (int s = 0; s < p.slabs; ++s) {
-            const float d = q[(int64_t)s * a.G * 2] - mean;
-            m2 += q[(int64_t)s * a.G * 2 + 1] +
-                  (float)min(p.px, a.P - s * p.px) * (float)cpg * d * d;
-        }
-        stat[2 * (g - g0)] = mean;
-        stat[2 * (g - g0) + 1] = 1.0f / sqrtf(m2 / ((float)a.P * (float)cpg) + a.eps);
-    }
-    __syncthreads();
     const int step = APPLY_NT / cols, slot = tid / cols, col = tid - slot * cols;
-    if (slot >= step || col >= nc) return;
-    float mean[V], ga[V], be[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int c = (ct * cols + col) * V + e, g = c / cpg - g0;
-        mean[e] = stat[2 * g];
-        ga[e] = stat[2 * g + 1] * (a.gamma ? a.gamma[c] : 1.0f);
-        be[e] = a.beta ? a.beta[c] : 0.0f;
-    }
-    const int first = rt * rows, last = min(a.P, first + rows);
+    const int first = rt * rows, last = slot >= step || col >= nc ? 0 : min(a.P, first + rows);
     const int64_t at = (int64_t)n * a.P * CV + ct * cols + col;
     const uint4* x = (const uint4*)a.x + at;
     uint4* y = (uint4*)a.y + at;
+    // first vectors, scales and shifts on their way while the statistics are joined
     constexpr int B = 4;
-    for (int q = first + slot; q < last; q += B * step) {
-        uint4 u[B];
+    uint4 u[B];
+    auto load = [&](int q) {
 #pragma unroll
         for (int b = 0; b < B; ++b)
             if (q + b * step < last) u[b] = x[(int64_t)(q + b * step) * CV];
+    };
+    load(first + slot);
+    float mean[V], ga[V], be[V];
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-            if (q + b * step >= last) break;
-            float v[V];
-            unpack<T, V>(u[b], v);
+    for (int e = 0; e < V; ++e) {
+        const int c = (ct * cols + min(col, nc - 1)) * V + e;
+        ga[e] = a.gamma ? a.gamma[c] : 1.0f;
+        be[e] = a.beta ? a.beta[c] : 0.0f;
+    }
+    const int g0 = ct * cols * V / cpg, g1 = (ct * cols * V + nc * V - 1) / cpg;
+    // eight lanes a group: each joins every eighth slab, then they join each other
+    // (n = pixels; the differences' sums are of pixels x channels)
+    auto join = [&](float& n0, float& mean0, float& m20, float n1, float mean1, float m21) {
+        const float both = n0 + n1, d = mean1 - mean0, w = both > 0.0f ? n1 / both : 0.0f;
+        m20 += n1 > 0.0f ? m21 + d * d * n0 * w * (float)cpg : 0.0f;
+        mean0 += n1 > 0.0f ? d * w : 0.0f;
+        n0 = both;
+    };
+    for (int gb = g0; gb <= g1; gb += APPLY_NT / 8) {
+        const int g = min(gb + tid / 8, g1);
+        const float* q = part + ((int64_t)n * p.slabs * a.G + g) * 2;
+        float cnt = 0.0f, mean = 0.0f, m2 = 0.0f;
+#pragma unroll 4
+        for (int s = tid % 8; s < p.slabs; s += 8) {
+            const float2 v = *(const float2*)(q + (int64_t)s * a.G * 2);
+            join(cnt, mean, m2, (float)min(p.px, a.P - s * p.px), v.x, v.y);
+        }
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                v[e] = norm_act(__builtin_fmaf(v[e] - mean[e], ga[e], be[e]), a.act);
-            y[(int64_t)(q + b * step) * CV] = pack<T, V>(v);
+        for (int m = 1; m < 8; m *= 2)
+            join(cnt, mean, m2, __shfl_xor(cnt, m), __shfl_xor(mean, m), __shfl_xor(m2, m));
+        if (tid % 8 == 0 && gb + tid / 8 <= g1) {
+            stat[2 * (g - g0)] = mean;
+            stat[2 * (g - g0) + 1] = 1.0f / sqrtf(m2 / ((float)a.P * (float)cpg) + a.eps);
         }
     }
+    __syncthreads();
+    if (last == 0) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const int g = ((ct * cols + col) * V + e) / cpg - g0;
+        mean[e] = stat[2 * g];
+        ga[e] *= stat[2 * g + 1];
+        if constexpr (ESZ == 2) be[e] = __builtin_fmaf(-mean[e], ga[e], be[e]);
+    }
+    with_act(a.act, [&](auto act) {
+        for (int q = first + slot; q < last; q += B * step) {
+            if (q > first + slot) load(q);
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                if (q + b * step >= last) break;
+                float v[V];
+                unpack<T, V>(u[b], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    v[e] = norm_act<decltype(act)::value>(
+                        __builtin_fmaf(ESZ == 2 ? v[e] : v[e] - mean[e], ga[e], be[e]));
+                y[(int64_t)(q + b * step) * CV] = pack<T, V>(v);
+            }
+        }
+    });
 }
 
 template <typename T, int NT, int R>
 void launch_norm(const GroupNormArgs& a, const NormPlan& p, float* part, hipStream_t s)
 {
     const dim3 grid((uint32_t)((int64_t)a.N * p.slabs * p.chunks));
-    if (p.single) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, true>), grid, dim3(NT), 0, s, a, p, part);
-    else PPIPE_LAUNCH((group_norm_kernel<T, NT, R, false>), grid, dim3(NT), 0, s, a, p, part);
+    if (!p.single && !p.whole) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, MIXED>), grid, dim3(NT), 0, s, a, p, part);
+    else if (!p.single) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, SEVERAL>), grid, dim3(NT), 0, s, a, p, part);
+    else if (p.whole && p.cv <= NT) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ONE>), grid, dim3(NT), 0, s, a, p, part);
+    else if constexpr (R < NORM_R)
+        PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ANY>), grid, dim3(NT), 0, s, a, p, part);
 }
 
 template <typename T>
@@ -383,15 +535,15 @@ void launch_type(const GroupNormArgs& a, const NormPlan& p, float* part, int cus
                      0, s, a, p, part, cols, col_tiles, rows, row_tiles);
         return;
     }
-    if (p.nt == 256) {
+    if (p.nt != NORM_NT) {
         if (p.r == 1) launch_norm<T, 256, 1>(a, p, part, s);
         else if (p.r == 2) launch_norm<T, 256, 2>(a, p, part, s);
         else launch_norm<T, 256, 4>(a, p, part, s);
     } else {
-        if (p.r == 2) launch_norm<T, NORM_NT, 2>(a, p, part, s);
-        else if (p.r == 4) launch_norm<T, NORM_NT, 4>(a, p, part, s);
+        if (p.r == 4) launch_norm<T, NORM_NT, 4>(a, p, part, s);
         else if (p.r == 8) launch_norm<T, NORM_NT, 8>(a, p, part, s);
-        else launch_norm<T, NORM_NT, 16>(a, p, part, s);
+        else if (p.r == 16) launch_norm<T, NORM_NT, 16>(a, p, part, s);
+        else launch_norm<T, NORM_NT, 32>(a, p, part, s);
     }
 }
 
