@@ -117,13 +117,35 @@ __device__ __forceinline__ uint32_t sad(uint32_t a, uint32_t b, uint32_t c)
     return max(a, b) - min(a, b) + c;
 }
 
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float a, float b)
+__device__ __forceinline__ uint32_t word(const uint4& u, int w)
 {
-    const T e[2] = {(T)a, (T)b};
-    uint32_t u;
-    __builtin_memcpy(&u, e, 4);
-    return u;
+    return w == 0 ? u.x : w == 1 ? u.y : w == 2 ? u.z : u.w;
+}
+
+// Zero, or NaN if one of two 16-bit values is not finite.
+template <typename T> __device__ __forceinline__ float not_finite(uint32_t u)
+{
+    T e[2];
+    __builtin_memcpy(e, &u, 4);
+    return (float)e[0] * 0.0f + (float)e[1] * 0.0f;
+}
+
+// Two values rounded to a 16-bit type, and a + b + c of such a pair: the sum of
+// the weights as the products with the values see them.
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    typedef T pair __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){a, b}, pair));
+}
+template <typename T> __device__ __forceinline__ float add2(uint32_t u, float c)
+{
+    typedef T pair __attribute__((ext_vector_type(2)));
+    if constexpr (std::is_same<T, __bf16>::value)
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, u),
+                                               (pair){(T)1.0f, (T)1.0f}, c, false);
+    else
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(pair, u), (pair){(T)1.0f, (T)1.0f}, c, false);
 }
 
 // SPLITK: the waves of a block share one tile of rows and take key tiles in
@@ -133,7 +155,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
 template <typename T, int DP, int QT, bool SPLITK> struct AttentionTile {
     static constexpr int ESZ = (int)sizeof(T);
     static constexpr int CH = DP * ESZ / 16;                    // 16-byte vectors of a row
-    static constexpr int BK = SPLITK || 4 * 64 * DP * ESZ > 131072 ? 32 : 64;
+    static constexpr int BK = SPLITK || DP * ESZ > 256 * (ESZ / 2) ? 32 : 64;
     static constexpr int KT = BK / 32;
     static constexpr int POS = 64 * 3 * 4;                      // key positions of a tile
     static constexpr int STAGE = 2 * BK * DP * ESZ + POS;
@@ -311,35 +333,41 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
     constexpr int KX = CH % 8 == 0 ? 4 : 2;    // vector pairs that the swizzle mixes
     const int kswz = TL::kswz(col);
     const uint32_t kread = (uint32_t)(col * RB + ((half ^ kswz) * 16));
-    // 16-bit V: this lane's row and column of a transposing read
-    const int vrow = 4 * half + (lane % 16) / 4;
+    // 16-bit V: this lane's row and column of a transposing read, for even and
+    // odd blocks of 32 elements (the swizzle turns their order); fp32: its element
+    const int vrow = ESZ == 2 ? 4 * half + (lane % 16) / 4 : 4 * half;
     const int vcol = 2 * ((lane / 16) % 2) + (lane % 4) / 2;
+    uint32_t vread[2];
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+        vread[d] = KB + vrow * RB + (ESZ == 2 ? ((4 * d + vcol) ^ TL::vswz(vrow)) * 16 + (lane & 1) * 8
+                                              : 32 * d * 4 + col * 4);
 
-    if (ntiles > 0) load_tile(kbeg, 0);
-    for (int it = 0; it < ntiles; ++it) {
-        const int k0 = kbeg + it * STEP;
-        const uint32_t src = lds0 + (it & 1) * TL::STAGE;
-        dma_wait<0>();
-        lds_read_drain();
-        if constexpr (!SPLITK) bare_barrier();
-        if (it + 1 < ntiles) load_tile(k0 + STEP, (it + 1) & 1);
-        if (k0 >= whi || k0 + BK <= wlo) continue;             // no row of this wave sees it
-        const bool whole = k0 >= wlo_max && k0 + BK <= whi_min; // every row sees all of it
+    auto tile_pass = [&](int k0, uint32_t src, auto seen_whole) {
+        constexpr bool whole = decltype(seen_whole)::value;
+        // this stage's read addresses, held apart from the loop (the compiler would
+        // keep one for every read of both stages)
+        uint32_t kat[KX], vat[2];
+#pragma unroll
+        for (int c = 0; c < KX; ++c) kat[c] = src + (kread ^ (c * 32));
+#pragma unroll
+        for (int d = 0; d < 2; ++d) vat[d] = src + vread[d];
+#pragma unroll
+        for (int c = 0; c < KX; ++c) asm volatile("" : "+v"(kat[c]));
+        asm volatile("" : "+v"(vat[0]), "+v"(vat[1]));
 
         // ---- scores ----
         accx16 s[QT][KT];
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-            for (int k = 0; k < KT; ++k) s[t][k] = accx16{};
-#pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int c = 0; c < CH / 2; ++c) {
-                const uint4 kf = lds_read16(
-                    src + (kread ^ ((c % KX) * 32)) + (c / KX) * (32 * KX) + k * 32 * RB);
+                const uint4 kf = lds_read16(kat[c % KX] + (c / KX) * (32 * KX) + k * 32 * RB);
 #pragma unroll
-                for (int t = 0; t < QT; ++t) Mfma32<T>::step(kf, q[t][c], s[t][k]);
+                for (int t = 0; t < QT; ++t) {
+                    if (c == 0) s[t][k] = accx16{};
+                    Mfma32<T>::step(kf, q[t][c], s[t][k]);
+                }
             }
         if constexpr (EXTRA) {
 #pragma unroll
@@ -381,7 +409,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                         }
                 }
         }
-        if (!whole) {
+        if constexpr (!whole) {
 #pragma unroll
             for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -414,16 +442,13 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                 for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
             }
             const float base = M[t] == -INFINITY ? 0.0f : M[t];
-            float sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k][i], p.c, -base));
-                    s[t][k][i] = w;
-                    sum += w;
+                    s[t][k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k][i], p.c, -base));
+                    if constexpr (ESZ == 4) l[t] += s[t][k][i];
                 }
-            l[t] += sum;
             if constexpr (ESZ == 2)
 #pragma unroll
                 for (int k = 0; k < 2 * KT; ++k) {
@@ -432,6 +457,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                     // instruction takes both operands in it
                     pf[t][k] = make_uint4(pack2<T>(w(0), w(1)), pack2<T>(w(2), w(3)),
                                           pack2<T>(w(4), w(5)), pack2<T>(w(6), w(7)));
+                    l[t] = add2<T>(pf[t][k].w, add2<T>(pf[t][k].z, add2<T>(pf[t][k].y, add2<T>(pf[t][k].x, l[t]))));
                 }
         }
 
@@ -439,36 +465,37 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
         // Keys that only some rows see may hold NaN or infinities, and 0 x NaN
         // would reach the others: where a tile is not seen whole, non-finite
         // values are looked for and then added key by key, to their rows alone.
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            if constexpr (ESZ == 2) {
-                uint4 vf[2 * KT];
+        if constexpr (ESZ == 2) {
+            // values of the next 32 elements are read while these are multiplied
+            uint4 vf[2][2 * KT];
+            auto read_v = [&](int d, uint4* f) {
 #pragma unroll
                 for (int k = 0; k < 2 * KT; ++k) {
-                    const int ch = (4 * d + vcol) ^ TL::vswz(vrow);
-                    const uint32_t at = src + KB + (16 * k + vrow) * RB + ch * 16 + (lane & 1) * 8;
+                    const uint32_t at = vat[d & 1] + (d / 2) * 128 + 16 * k * RB;
                     const uint2 x = lds_read_columns(at), y = lds_read_columns(at + 8 * RB);
-                    vf[k] = make_uint4(x.x, x.y, y.x, y.y);
+                    f[k] = make_uint4(x.x, x.y, y.x, y.y);
                 }
+            };
+            read_v(0, vf[0]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const uint4* f = vf[d & 1];
+                __builtin_amdgcn_sched_barrier(0);
+                if (d + 1 < DT) read_v(d + 1, vf[(d + 1) & 1]);
                 bool clean = true;
-                if (!whole) {
+                if constexpr (!whole) {
                     float z = 0.0f;
 #pragma unroll
                     for (int k = 0; k < 2 * KT; ++k)
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const uint32_t u = w == 0 ? vf[k].x : w == 1 ? vf[k].y : w == 2 ? vf[k].z : vf[k].w;
-                            T e[2];
-                            __builtin_memcpy(e, &u, 4);
-                            z += (float)e[0] * 0.0f + (float)e[1] * 0.0f;
-                        }
+                        for (int w = 0; w < 4; ++w) z += not_finite<T>(word(f[k], w));
                     clean = !__any(!(z == 0.0f));
                 }
-                if (clean) {
+                if (whole || clean) {
 #pragma unroll
                     for (int k = 0; k < 2 * KT; ++k)
 #pragma unroll
-                        for (int t = 0; t < QT; ++t) Mfma32<T>::step(vf[k], pf[t][k], o[t][d]);
+                        for (int t = 0; t < QT; ++t) Mfma32<T>::step(f[k], pf[t][k], o[t][d]);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 2 * KT; ++k)
@@ -481,7 +508,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                                                   w == 2 ? u.z & m : 0u, w == 3 ? u.w & m : 0u);
                             };
                             const int j = k0 + 16 * k + 4 * (e / 8) + (e & 3) + 8 * ((e >> 2) & 1);
-                            const uint4 vk = only(vf[k]);
+                            const uint4 vk = only(f[k]);
 #pragma unroll
                             for (int t = 0; t < QT; ++t) {
                                 accx16 one = accx16{};
@@ -492,47 +519,82 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                             }
                         }
                 }
-            } else {
-                float vf[16 * KT];
+            }
+        } else {
+            // 16 keys and 32 elements at a time
 #pragma unroll
-                for (int k = 0; k < KT; ++k)
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    float vf[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        vf[16 * k + i] = lds_read_f32(
-                            src + KB + (32 * k + 8 * (i / 4) + 4 * half + i % 4) * RB + (32 * d + col) * 4);
-                bool clean = true;
-                if (!whole) {
-                    float z = 0.0f;
+                        vf[i] = lds_read_f32(vat[d & 1] + (d / 2) * 256 + (32 * k + 8 * (i / 4) + i % 4) * RB);
+                    bool clean = true;
+                    if constexpr (!whole) {
+                        float z = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 16 * KT; ++i) z += vf[i] * 0.0f;
-                    clean = !__any(!(z == 0.0f));
-                }
+                        for (int i = 0; i < 16; ++i) z += vf[i] * 0.0f;
+                        clean = !__any(!(z == 0.0f));
+                    }
+                    if (whole || clean) {
 #pragma unroll
-                for (int k = 0; k < KT; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (clean) {
+                        for (int i = 0; i < 16; ++i)
 #pragma unroll
                             for (int t = 0; t < QT; ++t)
-                                o[t][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[16 * k + i], s[t][k][i],
-                                                                               o[t][d], 0, 0, 0);
-                        } else {
+                                o[t][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[i], s[t][k][i], o[t][d],
+                                                                               0, 0, 0);
+                    } else {
 #pragma unroll 1
-                            for (int e = 0; e < 2; ++e) {
-                                const int j = k0 + 32 * k + 8 * (i / 4) + 4 * e + i % 4;
+                        for (int x = 0; x < 32; ++x) {
+                            const int e = x / 16, i = x % 16;
+                            const int j = k0 + 32 * k + 8 * (i / 4) + 4 * e + i % 4;
+                            float v = 0.0f;
 #pragma unroll
-                                for (int t = 0; t < QT; ++t) {
-                                    const bool sees = j >= lo[t] && j < hi[t];
-                                    const accx16 one = __builtin_amdgcn_mfma_f32_32x32x2f32(
-                                        half == e ? vf[16 * k + i] : 0.0f, half == e ? s[t][k][i] : 0.0f,
-                                        accx16{}, 0, 0, 0);
+                            for (int y = 0; y < 16; ++y) v = y == i ? vf[y] : v;
 #pragma unroll
-                                    for (int x = 0; x < 16; ++x) o[t][d][x] += sees ? one[x] : 0.0f;
-                                }
+                            for (int t = 0; t < QT; ++t) {
+                                float w = 0.0f;
+#pragma unroll
+                                for (int y = 0; y < 16; ++y) w = y == i ? s[t][k][y] : w;
+                                const bool sees = j >= lo[t] && j < hi[t];
+                                const accx16 one = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                                    half == e ? v : 0.0f, half == e ? w : 0.0f, accx16{}, 0, 0, 0);
+#pragma unroll
+                                for (int y = 0; y < 16; ++y) o[t][d][y] += sees ? one[y] : 0.0f;
                             }
                         }
                     }
-            }
+                }
+        }
+    };
+
+    // waits for tile `it`, sends the next one's loads, gives the tile's first key
+    auto next_tile = [&](int it) {
+        dma_wait<0>();
+        lds_read_drain();
+        if constexpr (!SPLITK) bare_barrier();
+        const int k0 = kbeg + it * STEP;
+        if (it + 1 < ntiles) load_tile(k0 + STEP, (it + 1) & 1);
+        return k0;
+    };
+    // A tile that every row sees whole needs no mask and no care for its values.
+    // Runs of such tiles have a loop of their own, in which the accumulators stay
+    // where they are.
+    auto whole = [&](int it) {
+        const int k0 = kbeg + it * STEP;
+        return k0 >= wlo_max && k0 + BK <= whi_min;
+    };
+    if (ntiles > 0) load_tile(kbeg, 0);
+    for (int it = 0; it < ntiles;) {
+        for (; it < ntiles && !whole(it); ++it) {
+            const int k0 = next_tile(it);
+            if (k0 < whi && k0 + BK > wlo)                     // some row of this wave sees it
+                tile_pass(k0, lds0 + (it & 1) * TL::STAGE, std::false_type{});
+        }
+        for (; it < ntiles && whole(it); ++it) {
+            const int k0 = next_tile(it);
+            tile_pass(k0, lds0 + (it & 1) * TL::STAGE, std::true_type{});
         }
     }
 
