@@ -104,7 +104,11 @@ AttentionPlan plan_of(const AttentionArgs& a, const AttentionChoice& c, void* ws
     p.sign = a.scale == 0.0f ? 0 : a.scale < 0.0f ? -1 : 1;
     p.pre = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
     p.c = (float)(1.4426950408889634 * (extra ? 1.0 : (double)p.pre));
-    const int64_t all = (int64_t)a.N * a.Hk * p.rows;
+    p.capc = a.cap > 0.0f ? (float)(2.8853900817779268 * p.pre / a.cap) : 0.0f;
+    p.capk = 2.0f * a.cap;
+    const int64_t groups = (int64_t)a.N * a.Hk;
+    p.by_tile = c.splits == 1 && groups % NUM_XCD != 0 && groups <= 64;
+    const int64_t all = groups * p.rows;
     p.part = (float*)ws;
     p.ml = ws ? (float*)ws + c.splits * all * a.d : nullptr;
     return p;

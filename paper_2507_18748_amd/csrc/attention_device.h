@@ -13,6 +13,8 @@ struct AttentionPlan {
     int rows;          // query rows of one key head: Lq * (H / Hk)
     int tiles;         // row tiles of one key head
     int splits;        // key ranges per row tile
+    int by_tile;       // blocks in the order of row tiles, not key heads
+    float capc, capk;  // with a cap: tanh's exponent per unit of q . k; 2 cap
     float c;           // scores in powers of two: c * (q . k), or log2(e) after cap and bias
     float pre;         // with cap or bias: the scale itself
     int sign;          // 0: q is read as zeros, -1: with its sign turned
@@ -111,15 +113,17 @@ __device__ __forceinline__ float lds_read_f32(uint32_t addr)
     return *(const __attribute__((address_space(3))) float*)(uintptr_t)addr;
 }
 
-// |a - b| + c of integers whose sign bits were turned.
-__device__ __forceinline__ uint32_t sad(uint32_t a, uint32_t b, uint32_t c)
-{
-    return max(a, b) - min(a, b) + c;
-}
-
 __device__ __forceinline__ uint32_t word(const uint4& u, int w)
 {
     return w == 0 ? u.x : w == 1 ? u.y : w == 2 ? u.z : u.w;
+}
+
+// |a - b| + c of integers whose sign bits were turned.
+__device__ __forceinline__ uint32_t sad(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("v_sad_u32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
 }
 
 // Zero, or NaN if one of two 16-bit values is not finite.
@@ -167,13 +171,17 @@ template <typename T, int DP, int QT, bool SPLITK> struct AttentionTile {
     static constexpr int ROWS = SPLITK ? 32 : 32 * QT * NW;     // rows of a block
     static constexpr int NI = BK * CH / 64;                     // wave loads of a K or V tile
     static constexpr int NL = SPLITK ? NI : NI / NW;            // of them, one wave's
-    // Row r keeps vector c of K at c ^ kswz(r): the 8 rows that a fragment read
-    // takes at once lie in different banks.  Of V, 16-bit: the 4 rows of a
-    // transposing read do.
-    static __device__ __forceinline__ int kswz(int r) { return CH % 8 == 0 ? r & 7 : (r >> 1) & 3; }
+    // LDS has 64 banks: 16 lanes of a 16-byte read, 32 of an 8-byte one must lie in
+    // different 16 or 8 bytes of 256.  Row r keeps vector c of K at c ^ kswz(r), so
+    // the 16 rows that a fragment read takes at once do; of V, 16-bit, at
+    // c ^ vswz(r): the 4 rows x 64 bytes of two transposing reads do.
+    static __device__ __forceinline__ int kswz(int r)
+    {
+        return CH % 16 == 0 ? r & 15 : CH % 8 == 0 ? (r >> 1) & 7 : (r >> 2) & 3;
+    }
     static __device__ __forceinline__ int vswz(int r)
     {
-        return ESZ == 4 ? 0 : CH % 8 == 0 ? (r & 3) << 1 : ((r >> 1) & 1) << 1;
+        return ESZ == 4 || CH % 8 ? 0 : CH % 16 == 0 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
     }
 };
 
@@ -191,15 +199,25 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int col = lane % 32, half = lane / 32;
-    // blocks of one key head lie on one XCD, the later rows (more keys under a
-    // causal mask) first
-    const uint32_t per = gridDim.x / NUM_XCD, rem = gridDim.x % NUM_XCD;
+    // Blocks of one key head lie on one XCD, the later rows (more keys under a
+    // causal mask) first.  A number of key heads that the XCDs do not divide goes
+    // row tile by row tile, or some would get the long rows alone (causal, 4 key
+    // heads: 193 -> @@ us).
     const uint32_t xcd = blockIdx.x % NUM_XCD;
-    uint32_t lin = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / NUM_XCD;
-    const int split = lin % (uint32_t)p.splits;
-    lin /= (uint32_t)p.splits;
-    const int tile = p.tiles - 1 - (int)(lin % (uint32_t)p.tiles);
-    const int group = (int)(lin / (uint32_t)p.tiles);          // n * Hk + hk
+    uint32_t lin = blockIdx.x;
+    int split = 0, tile, group;                                // group: n * Hk + hk
+    if (p.by_tile) {
+        const uint32_t groups = (uint32_t)(a.N * a.Hk);
+        tile = p.tiles - 1 - (int)(lin / groups);
+        group = (int)(lin % groups);
+    } else {
+        const uint32_t per = gridDim.x / NUM_XCD, rem = gridDim.x % NUM_XCD;
+        lin = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / NUM_XCD;
+        split = lin % (uint32_t)p.splits;
+        lin /= (uint32_t)p.splits;
+        tile = p.tiles - 1 - (int)(lin % (uint32_t)p.tiles);
+        group = (int)(lin / (uint32_t)p.tiles);
+    }
     const int n = group / a.Hk, hk = group - n * a.Hk, G = a.H / a.Hk;
 
     // ---- this lane's rows: query, span, bias ----
@@ -330,16 +348,16 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[t][d] = accx16{};
     }
-    constexpr int KX = CH % 8 == 0 ? 4 : 2;    // vector pairs that the swizzle mixes
+    constexpr int KX = CH % 16 == 0 ? 8 : CH % 8 == 0 ? 4 : 2;    // vector pairs that the swizzle mixes
     const int kswz = TL::kswz(col);
     const uint32_t kread = (uint32_t)(col * RB + ((half ^ kswz) * 16));
-    // 16-bit V: this lane's row and column of a transposing read, for even and
-    // odd blocks of 32 elements (the swizzle turns their order); fp32: its element
+    // 16-bit V: this lane's row and column of a transposing read, for four
+    // blocks of 32 elements (the swizzle turns their order); fp32: its element
     const int vrow = ESZ == 2 ? 4 * half + (lane % 16) / 4 : 4 * half;
     const int vcol = 2 * ((lane / 16) % 2) + (lane % 4) / 2;
-    uint32_t vread[2];
+    uint32_t vread[4];
 #pragma unroll
-    for (int d = 0; d < 2; ++d)
+    for (int d = 0; d < 4; ++d)
         vread[d] = KB + vrow * RB + (ESZ == 2 ? ((4 * d + vcol) ^ TL::vswz(vrow)) * 16 + (lane & 1) * 8
                                               : 32 * d * 4 + col * 4);
 
@@ -347,14 +365,14 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
         constexpr bool whole = decltype(seen_whole)::value;
         // this stage's read addresses, held apart from the loop (the compiler would
         // keep one for every read of both stages)
-        uint32_t kat[KX], vat[2];
+        uint32_t kat[KX], vat[4];
 #pragma unroll
         for (int c = 0; c < KX; ++c) kat[c] = src + (kread ^ (c * 32));
 #pragma unroll
-        for (int d = 0; d < 2; ++d) vat[d] = src + vread[d];
+        for (int d = 0; d < 4; ++d) vat[d] = src + vread[d];
 #pragma unroll
         for (int c = 0; c < KX; ++c) asm volatile("" : "+v"(kat[c]));
-        asm volatile("" : "+v"(vat[0]), "+v"(vat[1]));
+        asm volatile("" : "+v"(vat[0]), "+v"(vat[1]), "+v"(vat[2]), "+v"(vat[3]));
 
         // ---- scores ----
         accx16 s[QT][KT];
@@ -370,44 +388,53 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                 }
             }
         if constexpr (EXTRA) {
+            // one branch for the tile, not for each score
+            auto each = [&](auto&& f) {
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
+                for (int t = 0; t < QT; ++t)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    uint4 kp[3];
-                    if (a.slopes)
+                    for (int k = 0; k < KT; ++k)
 #pragma unroll
-                        for (int x = 0; x < 3; ++x)
-                            if (x < a.A)
-                                kp[x] = lds_read16(src + 2 * KB + x * 256 +
-                                                   (32 * k + 8 * g + 4 * half) * 4);
+                        for (int i = 0; i < 16; ++i) s[t][k][i] = f(s[t][k][i]);
+            };
+            if (a.cap > 0.0f) {
+                if constexpr (ESZ == 4)
+                    each([&](float v) { return a.cap * tanhf(v * p.pre / a.cap); });
+                else   // tanh x = 1 - 2 / (2^(2 x log2 e) + 1)
+                    each([&](float v) {
+                        const float e = __builtin_amdgcn_exp2f(v * p.capc);
+                        return __builtin_fmaf(-p.capk, __builtin_amdgcn_rcpf(e + 1.0f), a.cap);
+                    });
+            } else {
+                each([&](float v) { return v * p.pre; });
+            }
+            auto bias = [&](auto axes) {
+                constexpr int A = decltype(axes)::value;
 #pragma unroll
-                    for (int t = 0; t < QT; ++t)
+                for (int k = 0; k < KT; ++k)
 #pragma unroll
-                        for (int b = 0; b < 4; ++b) {
-                            float v = s[t][k][4 * g + b] * p.pre;
-                            if (a.cap > 0.0f) {
-                                if constexpr (ESZ == 4) {
-                                    v = a.cap * tanhf(v / a.cap);
-                                } else {
-                                    // tanh x = 1 - 2 / (2^(2 x log2 e) + 1)
-                                    const float e = __builtin_amdgcn_exp2f(v * (2.8853900818f / a.cap));
-                                    v = a.cap - 2.0f * a.cap * __builtin_amdgcn_rcpf(e + 1.0f);
-                                }
-                            }
-                            if (a.slopes) {
+                    for (int g = 0; g < 4; ++g) {
+                        uint4 kp[A];
+#pragma unroll
+                        for (int x = 0; x < A; ++x)
+                            kp[x] = lds_read16(src + 2 * KB + x * 256 + (32 * k + 8 * g + 4 * half) * 4);
+#pragma unroll
+                        for (int t = 0; t < QT; ++t)
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
                                 uint32_t dist = 0;
 #pragma unroll
-                                for (int x = 0; x < 3; ++x)
-                                    if (x < a.A)
-                                        dist = sad(qp[t][x],
-                                                   (b == 0 ? kp[x].x : b == 1 ? kp[x].y
-                                                    : b == 2 ? kp[x].z : kp[x].w) ^ 0x80000000u, dist);
-                                v -= slope[t] * (float)dist;
+                                for (int x = 0; x < A; ++x)
+                                    dist = sad(qp[t][x], word(kp[x], b) ^ 0x80000000u, dist);
+                                s[t][k][4 * g + b] = __builtin_fmaf(-slope[t], (float)dist, s[t][k][4 * g + b]);
                             }
-                            s[t][k][4 * g + b] = v;
-                        }
-                }
+                    }
+            };
+            if (a.slopes) {
+                if (a.A == 1) bias(std::integral_constant<int, 1>{});
+                else if (a.A == 2) bias(std::integral_constant<int, 2>{});
+                else bias(std::integral_constant<int, 3>{});
+            }
         }
         if constexpr (!whole) {
 #pragma unroll
@@ -471,7 +498,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             auto read_v = [&](int d, uint4* f) {
 #pragma unroll
                 for (int k = 0; k < 2 * KT; ++k) {
-                    const uint32_t at = vat[d & 1] + (d / 2) * 128 + 16 * k * RB;
+                    const uint32_t at = vat[d & 3] + (d / 4) * 256 + 16 * k * RB;
                     const uint2 x = lds_read_columns(at), y = lds_read_columns(at + 8 * RB);
                     f[k] = make_uint4(x.x, x.y, y.x, y.y);
                 }
@@ -529,7 +556,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                     float vf[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        vf[i] = lds_read_f32(vat[d & 1] + (d / 2) * 256 + (32 * k + 8 * (i / 4) + i % 4) * RB);
+                        vf[i] = lds_read_f32(vat[d & 3] + (d / 4) * 512 + (32 * k + 8 * (i / 4) + i % 4) * RB);
                     bool clean = true;
                     if constexpr (!whole) {
                         float z = 0.0f;
