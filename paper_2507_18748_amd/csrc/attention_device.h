@@ -339,6 +339,17 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             }
     };
 
+    // the queries (and their positions) are here before the loop: else every tile would wait for all
+    // loads under way, the next tile's among them, before its first product
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+#pragma unroll
+        for (int c = 0; c < CH / 2; ++c)
+            asm volatile("" : "+v"(q[t][c].x), "+v"(q[t][c].y), "+v"(q[t][c].z), "+v"(q[t][c].w));
+        if constexpr (EXTRA)
+            asm volatile("" : "+v"(slope[t]), "+v"(qp[t][0]), "+v"(qp[t][1]), "+v"(qp[t][2]));
+    }
+
     accx16 o[QT][DT];
     float M[QT], l[QT];
 #pragma unroll
@@ -387,6 +398,18 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                     Mfma32<T>::step(kf, q[t][c], s[t][k]);
                 }
             }
+        // six reads ahead of the products (two, the compiler's choice, leave each
+        // product waiting for LDS)
+        {
+            constexpr int N = KT * (CH / 2), PER = QT * (ESZ == 4 ? 4 : 1), AHEAD = N < 6 ? N : 6;
+            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+            for (int i = 0; i < N - AHEAD; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * PER, 0);
+        }
         if constexpr (EXTRA) {
             // one branch for the tile, not for each score
             auto each = [&](auto&& f) {
