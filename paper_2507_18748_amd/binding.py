@@ -7,6 +7,7 @@ built: there is no fallback implementation.
 """
 import ctypes
 import os
+import struct
 from typing import Dict, Iterable, List, Optional, Sequence
 
 import numpy as np
@@ -74,6 +75,14 @@ class AttentionDesc(ctypes.Structure):
                 ("q_strides", _i64x3), ("k_strides", _i64x3), ("v_strides", _i64x3),
                 ("out_strides", _i64x3), ("q_positions_stride", ctypes.c_int64),
                 ("k_positions_stride", ctypes.c_int64), ("spans_stride", ctypes.c_int64)]
+
+
+# The same two descriptions packed for one call (filling a Structure takes
+# longer than the launch it describes).
+_ROTARY = struct.Struct("@11id3q3qq")
+_ATTENTION = struct.Struct("@7i2fi12q3q")
+assert _ROTARY.size == ctypes.sizeof(RotaryDesc)
+assert _ATTENTION.size == ctypes.sizeof(AttentionDesc)
 
 
 def _records(recs, count: int, cap: int) -> List[dict]:
@@ -219,14 +228,13 @@ def load_library() -> ctypes.CDLL:
     lib.ppipe_group_norm.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, f32, i32, vp, i64,
                                      vp]
     lib.ppipe_rotary.restype = ctypes.c_int
-    lib.ppipe_rotary.argtypes = [ctypes.POINTER(RotaryDesc), vp, vp, vp, vp]
+    lib.ppipe_rotary.argtypes = [vp, vp, vp, vp, vp]
     lib.ppipe_attention_spans.restype = ctypes.c_int
     lib.ppipe_attention_spans.argtypes = [vp, i32, i32, i32, vp, i32, vp, i32, vp, vp]
     lib.ppipe_attention_workspace.restype = i64
     lib.ppipe_attention_workspace.argtypes = [ctypes.POINTER(AttentionDesc)]
     lib.ppipe_attention.restype = ctypes.c_int
-    lib.ppipe_attention.argtypes = [ctypes.POINTER(AttentionDesc), vp, vp, vp, vp, vp, vp, vp,
-                                    vp, vp, i64, vp]
+    lib.ppipe_attention.argtypes = [vp] * 10 + [i64, vp]
     lib.ppipe_split_points.restype = ctypes.c_int
     lib.ppipe_split_points.argtypes = [ctypes.POINTER(ModelDesc), ctypes.POINTER(i32)]
     lib.ppipe_prepartition.restype = ctypes.c_int
@@ -324,10 +332,10 @@ def rotary(x_ptr: int, y_ptr: int, dtype: str, batch: int, tokens: int, heads: i
     axes = len(pairs)
     if axes > 3:
         raise PpipeError(-1, "rotary takes one to three axes")
-    desc = RotaryDesc(DTYPES[dtype], batch, tokens, heads, head_dim, axes,
-                      (ctypes.c_int32 * 3)(*pairs), bool(shared), bool(adjacent), base,
-                      _i64x3(*x_strides), _i64x3(*y_strides), positions_stride)
-    status = lib.ppipe_rotary(ctypes.byref(desc), x_ptr, positions_ptr, y_ptr, stream)
+    desc = _ROTARY.pack(DTYPES[dtype], batch, tokens, heads, head_dim, axes, *pairs,
+                        *(0,) * (3 - axes), bool(shared), bool(adjacent), base, *x_strides,
+                        *y_strides, positions_stride)
+    status = lib.ppipe_rotary(desc, x_ptr, positions_ptr, y_ptr, stream)
     if status != 0:
         raise _err(lib, status)
 
@@ -376,10 +384,10 @@ def attention(q_ptr: int, k_ptr: int, v_ptr: int, out_ptr: int, dtype: str, batc
     """Attention over strided [batch][token][head][head_dim] tensors (ppipe_attention):
     optional score cap, distance bias (slopes and positions) and spans of visible keys."""
     lib = load_library()
-    desc = attention_desc(dtype, batch, q_len, kv_len, heads, kv_heads, head_dim, q_strides,
-                          k_strides, v_strides, out_strides, scale, softcap, axes,
-                          q_positions_stride, k_positions_stride, spans_stride)
-    status = lib.ppipe_attention(ctypes.byref(desc), q_ptr, k_ptr, v_ptr, out_ptr, slopes_ptr,
+    desc = _ATTENTION.pack(DTYPES[dtype], batch, q_len, kv_len, heads, kv_heads, head_dim, scale,
+                           softcap, axes, *q_strides, *k_strides, *v_strides, *out_strides,
+                           q_positions_stride, k_positions_stride, spans_stride)
+    status = lib.ppipe_attention(desc, q_ptr, k_ptr, v_ptr, out_ptr, slopes_ptr,
                                  q_positions_ptr, k_positions_ptr, spans_ptr, workspace_ptr,
                                  workspace_bytes, stream)
     if status != 0:

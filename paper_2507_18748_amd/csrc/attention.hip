@@ -76,14 +76,20 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a, At
     Vec4<T>::store(y, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
 }
 
-// Rows of one key head up to 32: the waves of a block split the keys, and the
-// keys are split further among blocks until the chip is filled; each part keeps at
-// least 512 keys.
-AttentionChoice choose(int, const AttentionArgs& a, int cus)
+// Rows of one key head up to 32, or so few that blocks of 32 rows all run at once
+// (two to a CU up to 128 bytes of head, else one, by their LDS): the waves of a
+// block split the keys.  Measured, rows split / keys split (8 heads, us): 14x14
+// maps f32 of 32 x 3 16.1 / 8.5, bf16 of 64 x 1 9.1 / 7.7, x 4 9.3 / 8.0, 32x32 maps of 64 x 2
+// 18.6 / 15.8, f32 of 64 x 1 76 / 36; beyond one round: 32x32 of 128 x 3 27.6 / 45.6,
+// 14x14 of 32 x 16 8.0 / 11.6.
+// Few blocks: the keys are split further among blocks until the chip is filled; each part keeps
+// at least 512 keys.
+AttentionChoice choose(int dt, const AttentionArgs& a, int cus)
 {
     AttentionChoice c;
     const int64_t rows = (int64_t)a.Lq * (a.H / a.Hk), groups = (int64_t)a.N * a.Hk;
-    c.splitk = rows <= 32;
+    c.splitk = rows <= 32 || groups * ((rows + 31) / 32) <=
+                                 (int64_t)cus * (a.d * dtype_size(dt) <= 128 ? 2 : 1);
     const int per = c.splitk ? 32 : 128;
     c.tiles = (int)((rows + per - 1) / per);
     c.splits = 1;
@@ -94,18 +100,30 @@ AttentionChoice choose(int, const AttentionArgs& a, int cus)
     return c;
 }
 
-AttentionPlan plan_of(const AttentionArgs& a, const AttentionChoice& c, void* ws)
+AttentionPlan plan_of(int dt, const AttentionArgs& a, const AttentionChoice& c, void* ws)
 {
     AttentionPlan p;
     p.rows = a.Lq * (a.H / a.Hk);
     p.tiles = c.tiles;
     p.splits = c.splits;
-    const bool extra = a.cap > 0.0f || a.slopes;
+    // The scale goes into the exponent where it can: with a bias and no cap the
+    // slopes are divided by it (a scale beyond 2^+-40 multiplies the scores instead).
+    constexpr double LOG2E = 1.4426950408889634;
     p.sign = a.scale == 0.0f ? 0 : a.scale < 0.0f ? -1 : 1;
-    p.pre = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
-    p.c = (float)(1.4426950408889634 * (extra ? 1.0 : (double)p.pre));
-    p.capc = a.cap > 0.0f ? (float)(2.8853900817779268 * p.pre / a.cap) : 0.0f;
+    const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
+    const bool fold = scale > 0x1p-40f && scale < 0x1p40f;
+    p.capc = a.cap > 0.0f ? (float)(2.0 * LOG2E * scale / a.cap) : 0.0f;
     p.capk = 2.0f * a.cap;
+    p.pre = scale;
+    p.slope = 1.0f;
+    p.c = (float)LOG2E;
+    if (a.cap > 0.0f && !a.slopes && dt != DT_F32) {
+        p.c = (float)(LOG2E * p.capk);
+    } else if (a.cap == 0.0f && (fold || !a.slopes)) {
+        p.pre = 1.0f;
+        p.slope = 1.0f / scale;
+        p.c = (float)(LOG2E * scale);
+    }
     const int64_t groups = (int64_t)a.N * a.Hk;
     p.by_tile = c.splits == 1 && groups % NUM_XCD != 0 && groups <= 64;
     const int64_t all = groups * p.rows;
@@ -152,7 +170,7 @@ hipError_t launch_attention(int dt, const AttentionArgs& a, void* ws, int cus, i
                             hipStream_t s)
 {
     const AttentionChoice c = choose(dt, a, cus);
-    const AttentionPlan p = plan_of(a, c, ws);
+    const AttentionPlan p = plan_of(dt, a, c, ws);
     if (launch == 1) {
         const int64_t n = (int64_t)a.N * a.Lq * a.H * (a.d / 4);
         const dim3 grid((uint32_t)((n + 255) / 256)), block(256);

@@ -15,8 +15,9 @@ struct AttentionPlan {
     int splits;        // key ranges per row tile
     int by_tile;       // blocks in the order of row tiles, not key heads
     float capc, capk;  // with a cap: tanh's exponent per unit of q . k; 2 cap
-    float c;           // scores in powers of two: c * (q . k), or log2(e) after cap and bias
-    float pre;         // with cap or bias: the scale itself
+    float c;           // powers of two per unit of the scores as they are kept
+    float pre;         // factor of the scores before a bias
+    float slope;       // factor of the slopes
     int sign;          // 0: q is read as zeros, -1: with its sign turned
     float* part;       // [splits][N * Hk * rows][d] sums and [..][2] maxima and weights
     float* ml;
@@ -261,7 +262,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             whi_min = min(whi_min, hi[t]);
         }
         if constexpr (EXTRA) {
-            slope[t] = a.slopes && ok ? a.slopes[h] : 0.0f;
+            slope[t] = a.slopes && ok ? a.slopes[h] * p.slope : 0.0f;
 #pragma unroll
             for (int x = 0; x < 3; ++x)
                 qp[t][x] = a.slopes && ok && x < a.A
@@ -423,12 +424,18 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             if (a.cap > 0.0f) {
                 if constexpr (ESZ == 4)
                     each([&](float v) { return a.cap * tanhf(v * p.pre / a.cap); });
-                else   // tanh x = 1 - 2 / (2^(2 x log2 e) + 1)
+                else if (!a.slopes)
+                    // cap tanh x = cap - 2 cap / (2^(2 x log2 e) + 1): the constant drops
+                    // out of the softmax, and the factor is p.c's
+                    each([&](float v) {
+                        return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(v * p.capc));
+                    });
+                else
                     each([&](float v) {
                         const float e = __builtin_amdgcn_exp2f(v * p.capc);
                         return __builtin_fmaf(-p.capk, __builtin_amdgcn_rcpf(e + 1.0f), a.cap);
                     });
-            } else {
+            } else if (p.pre != 1.0f) {
                 each([&](float v) { return v * p.pre; });
             }
             auto bias = [&](auto axes) {
