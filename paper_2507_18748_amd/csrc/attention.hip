@@ -14,6 +14,8 @@
 // head fastest, 32 to a wave, so that few tokens with many heads fill a tile.
 #include "attention_device.h"
 
+#include <algorithm>
+
 namespace ppipe {
 namespace {
 
@@ -61,11 +63,13 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a, At
     float w = 0.0f;
     float4 sum = make_float4(0, 0, 0, 0);
     for (int s = 0; s < p.splits; ++s) {
-        const float ms = p.ml[(s * all + row) * 2];
-        if (ms == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(ms - m);
+        // a part without weight counts nothing; one of NaN scores alone has no
+        // maximum but its weight
+        const float ws = p.ml[(s * all + row) * 2 + 1];
+        if (ws == 0.0f) continue;
+        const float f = __builtin_amdgcn_exp2f(p.ml[(s * all + row) * 2] - m);
         const float4 v = *(const float4*)(p.part + (s * all + row) * a.d + e);
-        w += p.ml[(s * all + row) * 2 + 1] * f;
+        w += ws * f;
         sum.x += v.x * f; sum.y += v.y * f; sum.z += v.z * f; sum.w += v.w * f;
     }
     const int64_t group = row / p.rows;
@@ -82,8 +86,10 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a, At
 // maps f32 of 32 x 3 16.1 / 8.5, bf16 of 64 x 1 9.1 / 7.7, x 4 9.3 / 8.0, 32x32 maps of 64 x 2
 // 18.6 / 15.8, f32 of 64 x 1 76 / 36; beyond one round: 32x32 of 128 x 3 27.6 / 45.6,
 // 14x14 of 32 x 16 8.0 / 11.6.
-// Few blocks: the keys are split further among blocks until the chip is filled; each part keeps
-// at least 512 keys.
+// Few blocks: the keys are split further among blocks until the chip is filled;
+// each part keeps at least 512 keys for what the join costs (fp32, whose tiles
+// take several times as long: 256 of heads of 64, 64 of 256; 32 and 512 keys
+// there: 500 tokens of 8 heads of 128 32.7 / 44.6 / 45.1 us).
 AttentionChoice choose(int dt, const AttentionArgs& a, int cus)
 {
     AttentionChoice c;
@@ -93,8 +99,9 @@ AttentionChoice choose(int dt, const AttentionArgs& a, int cus)
     const int per = c.splitk ? 32 : 128;
     c.tiles = (int)((rows + per - 1) / per);
     c.splits = 1;
+    const int part = dt == DT_F32 ? std::max(64, 256 * 64 / a.d) : 512;
     while (c.splitk && c.splits < 64 && groups * c.tiles * c.splits < 2 * cus &&
-           a.Lk / (c.splits * 2) >= 512)
+           a.Lk / (c.splits * 2) >= part)
         c.splits *= 2;
     c.blocks = groups * c.tiles * c.splits;
     return c;
@@ -117,7 +124,9 @@ AttentionPlan plan_of(int dt, const AttentionArgs& a, const AttentionChoice& c, 
     p.pre = scale;
     p.slope = 1.0f;
     p.c = (float)LOG2E;
-    if (a.cap > 0.0f && !a.slopes && dt != DT_F32) {
+    p.cap_mode = a.cap == 0.0f ? CAP_NONE
+                 : dt == DT_F32 || a.cap > 1024.0f ? CAP_EXACT : a.slopes ? CAP_SUM : CAP_ALONE;
+    if (p.cap_mode == CAP_ALONE) {
         p.c = (float)(LOG2E * p.capk);
     } else if (a.cap == 0.0f && (fold || !a.slopes)) {
         p.pre = 1.0f;

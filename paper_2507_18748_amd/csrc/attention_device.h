@@ -8,12 +8,19 @@ namespace ppipe {
 typedef float accx16 __attribute__((ext_vector_type(16)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
+// How scores are capped: cap tanh x = cap - 2 cap / (2^(2 x log2 e) + 1).
+// Alone, the constant drops out of the softmax and the factor is the
+// exponent's.  These two lose 2^-23 of the cap, which 16-bit weights bear up to a
+// cap of 1024; fp32 and larger caps take the exact form (16-bit: a series where x is small).
+enum CapMode { CAP_NONE = 0, CAP_ALONE = 1, CAP_SUM = 2, CAP_EXACT = 3 };
+
 // What a launch adds to the call's arguments.
 struct AttentionPlan {
     int rows;          // query rows of one key head: Lq * (H / Hk)
     int tiles;         // row tiles of one key head
     int splits;        // key ranges per row tile
     int by_tile;       // blocks in the order of row tiles, not key heads
+    int cap_mode;
     float capc, capk;  // with a cap: tanh's exponent per unit of q . k; 2 cap
     float c;           // powers of two per unit of the scores as they are kept
     float pre;         // factor of the scores before a bias
@@ -203,7 +210,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
     // Blocks of one key head lie on one XCD, the later rows (more keys under a
     // causal mask) first.  A number of key heads that the XCDs do not divide goes
     // row tile by row tile, or some would get the long rows alone (causal, 4 key
-    // heads: 193 -> @@ us).
+    // heads: 193 -> 132 us).
     const uint32_t xcd = blockIdx.x % NUM_XCD;
     uint32_t lin = blockIdx.x;
     int split = 0, tile, group;                                // group: n * Hk + hk
@@ -421,20 +428,28 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[t][k][i] = f(s[t][k][i]);
             };
-            if (a.cap > 0.0f) {
+            if (p.cap_mode == CAP_EXACT) {
                 if constexpr (ESZ == 4)
                     each([&](float v) { return a.cap * tanhf(v * p.pre / a.cap); });
-                else if (!a.slopes)
-                    // cap tanh x = cap - 2 cap / (2^(2 x log2 e) + 1): the constant drops
-                    // out of the softmax, and the factor is p.c's
-                    each([&](float v) {
-                        return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(v * p.capc));
-                    });
                 else
                     each([&](float v) {
+                        const float x = v * (p.pre / a.cap), y = x * x;
                         const float e = __builtin_amdgcn_exp2f(v * p.capc);
-                        return __builtin_fmaf(-p.capk, __builtin_amdgcn_rcpf(e + 1.0f), a.cap);
+                        const float far = __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(e + 1.0f), 1.0f);
+                        float near = __builtin_fmaf(y, -0.053968254f, 0.13333333f);
+                        near = __builtin_fmaf(y, near, -0.33333333f);
+                        near = __builtin_fmaf(x * y, near, x);
+                        return a.cap * (fabsf(x) < 0.125f ? near : far);
                     });
+            } else if (p.cap_mode == CAP_ALONE) {
+                each([&](float v) {
+                    return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(v * p.capc));
+                });
+            } else if (p.cap_mode == CAP_SUM) {
+                each([&](float v) {
+                    const float e = __builtin_amdgcn_exp2f(v * p.capc);
+                    return __builtin_fmaf(-p.capk, __builtin_amdgcn_rcpf(e + 1.0f), a.cap);
+                });
             } else if (p.pre != 1.0f) {
                 each([&](float v) { return v * p.pre; });
             }
@@ -498,7 +513,9 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
             }
-            const float base = M[t] == -INFINITY ? 0.0f : M[t];
+            // weights of f16 are kept 2^6 up (at most 2^14), away from its small end
+            constexpr float UP = std::is_same<T, _Float16>::value ? 6.0f : 0.0f;
+            const float base = (M[t] == -INFINITY ? 0.0f : M[t]) - UP;
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
@@ -726,8 +743,10 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             for (int v = 0; v < NW; ++v) top = fmaxf(top, ml[(v * 32 + rr) * 2]);
             float4 sum = make_float4(0, 0, 0, 0);
             for (int v = 0; v < NW; ++v) {
-                const float mv = ml[(v * 32 + rr) * 2];
-                w += mv == -INFINITY ? 0.0f : ml[(v * 32 + rr) * 2 + 1] * __builtin_amdgcn_exp2f(mv - top);
+                // a part without weight counts nothing; one of NaN scores alone
+                // has no maximum but its weight
+                const float wv = ml[(v * 32 + rr) * 2 + 1];
+                w += wv == 0.0f ? 0.0f : wv * __builtin_amdgcn_exp2f(ml[(v * 32 + rr) * 2] - top);
                 const float4 part = *(const float4*)&f[(v * 32 + rr) * DP + e];
                 sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
             }

@@ -102,7 +102,7 @@ enum NormMode {
 };
 
 // One launch or two.  A block alone takes about 4 us and 0.45 us for each vector
-// that a thread holds (fp32: 0.3), and blocks beyond one per CU come in turn; two
+// that a thread holds (fp32: 0.3; of several groups 2.2 times that), and blocks beyond one per CU come in turn; two
 // launches take about 9 us and three passes at 5 TB/s.  Measured both ways (one /
 // two, us): 64 x 56x56x256 bf16 55 / 67, 8 x the same 14.8 / 17.6, 2 x 9.9 / 11.6,
 // 64 x 14x14x1024 15.6 / 25, 32 x 40x40x96 17.8 / 21.6, 1 x 112x112x64 in 32
@@ -150,7 +150,8 @@ NormPlan norm_plan(int dt, int N, int P, int C, int G, int cus)
         for (p.r = 4; p.r < most && pixels(p, p.nt, p.r) < P; p.r *= 2) {}
     }
     const double rounds = (double)(((int64_t)N * p.chunks + cus - 1) / cus);
-    const double one = 4.0 + (esz == 2 ? 0.45 : 0.3) * ((double)P * p.cv / p.nt) * rounds;
+    const double each = (esz == 2 ? 0.45 : 0.3) * (p.single || p.whole ? 1.0 : 2.2);
+    const double one = 4.0 + each * ((double)P * p.cv / p.nt) * rounds;
     const double two = 9.0 + 3.0 * N * (double)P * C * esz / 5e6;
     p.px = P;
     p.slabs = 1;
@@ -514,8 +515,7 @@ void launch_norm(const GroupNormArgs& a, const NormPlan& p, float* part, hipStre
     if (!p.single && !p.whole) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, MIXED>), grid, dim3(NT), 0, s, a, p, part);
     else if (!p.single) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, SEVERAL>), grid, dim3(NT), 0, s, a, p, part);
     else if (p.whole && p.cv <= NT) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ONE>), grid, dim3(NT), 0, s, a, p, part);
-    else if constexpr (R < NORM_R)
-        PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ANY>), grid, dim3(NT), 0, s, a, p, part);
+    else PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ANY>), grid, dim3(NT), 0, s, a, p, part);
 }
 
 template <typename T>

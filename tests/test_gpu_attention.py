@@ -134,6 +134,74 @@ def test_cap(dtype, d, cap):
     case(dtype, 1, 80, 130, 2, 1, d, cap=cap, size=6.0)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [-0.125, 0.0, 1e-15, 2.0])
+@pytest.mark.parametrize("extra", ["none", "cap", "bias", "both"])
+@pytest.mark.parametrize("lq", [1, 70])
+def test_scales(dtype, scale, extra, lq):
+    lk = 130
+    q, k, v = tensors(dtype, 1, lq, lk, 2, 2, 64)
+    slopes, qpos, kpos = bias(2, lq, lk, 2) if extra in ("bias", "both") else (None, None, None)
+    cap = 7.0 if extra in ("cap", "both") else 0.0
+    out = call(q, k, v, torch.empty_like(q, memory_format=torch.contiguous_format), dtype, scale,
+               cap, slopes, qpos, kpos)
+    ref, bound = R.attention(q, k, v, scale, cap, slopes, qpos, kpos, dtype=dtype)
+    R.check(out, ref, bound, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("cap", [1000.0, 1e6, 1e30])
+@pytest.mark.parametrize("biased", [False, True])
+def test_large_caps_keep_the_scores(dtype, cap, biased):
+    """A cap far above the scores leaves them as they are: within a few roundings of
+    the score itself above 1024, and of the cap below."""
+    lq, lk = 60, 300
+    q, k, v = tensors(dtype, 1, lq, lk, 2, 1, 64, size=4.0)
+    slopes, qpos, kpos = bias(2, lq, lk, 1) if biased else (None, None, None)
+    out = call(q, k, v, torch.empty_like(q, memory_format=torch.contiguous_format), dtype, 0.125,
+               cap, slopes, qpos, kpos)
+    ref, bound = R.attention(q, k, v, 0.125, 0.0 if cap > 1024 else cap, slopes, qpos, kpos, dtype=dtype)
+    if cap > 1024:      # x^3 / 3 of x = score / cap: below 1e-9 of the score from 1e6 on
+        size = float((q.double().norm(dim=-1).max() * k.double().norm(dim=-1).max()) * 0.125)
+        bound = bound + 2 * size * (size / 1e6) ** 2 * float(v.abs().max())
+    R.check(out, ref, bound, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lk", [40, 900, 20000])
+def test_nan_queries_and_keys(dtype, lk):
+    """A NaN query gives NaN at any split of its keys, and so does one NaN among
+    the keys it sees; other heads and items do not notice."""
+    q, k, v = tensors(dtype, 2, 1, lk, 2, 2, 64)
+    k, v = k.contiguous(), v.contiguous()
+    clean = call(q, k, v, torch.empty_like(q, memory_format=torch.contiguous_format), dtype, 0.125)
+    q2 = q.clone()
+    q2[0, 0, 1, 3] = float("nan")
+    out = call(q2, k, v, torch.empty_like(clean), dtype, 0.125)
+    assert bool(torch.isnan(out[0, 0, 1]).all())
+    assert torch.equal(out[1], clean[1]) and torch.equal(out[0, 0, 0], clean[0, 0, 0])
+    k[1, lk // 3, 0, 0] = float("nan")
+    out = call(q, k, v, torch.empty_like(clean), dtype, 0.125)
+    assert bool(torch.isnan(out[1, 0, 0]).all())
+    assert torch.equal(out[0], clean[0]) and torch.equal(out[1, 0, 1], clean[1, 0, 1])
+
+
+@pytest.mark.parametrize("lk", [300, 40000])
+def test_many_small_weights(lk):
+    """One key of weight near one and thousands of e^-17 each: their sum is not
+    lost to the small end of f16."""
+    d = 32
+    q = torch.zeros(1, 1, 1, d, device="cuda", dtype=torch.float16)
+    k = torch.zeros(1, lk, 1, d, device="cuda", dtype=torch.float16)
+    q[..., 0], k[0, 7, 0, 0] = 1.0, 17.0
+    v = torch.ones(1, lk, 1, d, device="cuda", dtype=torch.float16)
+    v[0, 7] = 0.0
+    out = call(q, k, v, torch.empty_like(q), "f16", 1.0)
+    # each weight is rounded once: 2^6 e^-17 = 2.6e-6 has steps of 2^-24, half of one is 0.0114 of it
+    want = (lk - 1) * math.exp(-17) / (1 + (lk - 1) * math.exp(-17))
+    assert float((out.double() / want - 1).abs().max()) <= 2.0 ** -25 / (64 * math.exp(-17)) + 4 * R.U["f16"] + 2.0 ** -25 / want
+
+
 def test_far_positions_keep_their_distance():
     """Distances of 32-bit positions are exact before they are rounded to fp32."""
     slopes = torch.tensor([0.01, 1.0], device="cuda")

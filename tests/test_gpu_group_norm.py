@@ -49,6 +49,22 @@ def test_sizes(dtype, n, p, c, groups):
     case(dtype, n, p, c, groups, act="silu")
 
 
+@pytest.mark.parametrize("dtype,c,groups", [
+    ("f32", 65536, 1), ("f16", 65536, 1), ("bf16", 65536, 2), ("f32", 65532, 2), ("f32", 65532, 1),
+    ("f16", 65528, 2), ("f16", 65528, 8191), ("f32", 65536, 65536), ("bf16", 40000, 1),
+])
+@pytest.mark.parametrize("n,p", [(2, 1), (1, 5), (1, 700)])
+def test_rows_longer_than_a_block(dtype, c, groups, n, p):
+    case(dtype, n, p, c, groups, "relu")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("groups", [1, 3, 16, 48])
+@pytest.mark.parametrize("n,p", [(1, 9000), (1, 60000), (30, 2000), (300, 9)])
+def test_one_launch_and_two(dtype, groups, n, p):
+    case(dtype, n, p, 48, groups, "gelu")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("affine", [True, False])
