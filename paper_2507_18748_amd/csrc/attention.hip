@@ -51,25 +51,27 @@ __global__ void __launch_bounds__(256) attention_spans_kernel(SpansArgs a)
 // Parts of the splits brought to one maximum, added in split order and
 // normalised; a thread takes four elements of a row.
 template <typename T>
-__global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs a, AttentionPlan p)
+__global__ void __launch_bounds__(64) attention_join_kernel(AttentionArgs a, AttentionPlan p)
 {
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)a.N * a.Hk * p.rows;
+    const int64_t x = (int64_t)blockIdx.x * 64 + threadIdx.x, all = (int64_t)a.N * a.Hk * p.rows;
     const int quads = a.d / 4;
     const int64_t row = x / quads;
     const int e = 4 * (int)(x - row * quads);
     if (row >= all) return;
-    float m = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, p.ml[(s * all + row) * 2]);
-    float w = 0.0f;
+    const float2* ml = (const float2*)p.ml + row;
+    const float* part = p.part + row * a.d + e;
+    float m = -INFINITY, w = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ml[s * all].x);
     float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll 4
     for (int s = 0; s < p.splits; ++s) {
         // a part without weight counts nothing; one of NaN scores alone has no
         // maximum but its weight
-        const float ws = p.ml[(s * all + row) * 2 + 1];
-        if (ws == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f(p.ml[(s * all + row) * 2] - m);
-        const float4 v = *(const float4*)(p.part + (s * all + row) * a.d + e);
-        w += ws * f;
+        const float2 x = ml[s * all];
+        const float f = x.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(x.x - m);
+        const float4 v = *(const float4*)(part + s * all * a.d);
+        w += x.y * f;
         sum.x += v.x * f; sum.y += v.y * f; sum.z += v.z * f; sum.w += v.w * f;
     }
     const int64_t group = row / p.rows;
@@ -182,7 +184,7 @@ hipError_t launch_attention(int dt, const AttentionArgs& a, void* ws, int cus, i
     const AttentionPlan p = plan_of(dt, a, c, ws);
     if (launch == 1) {
         const int64_t n = (int64_t)a.N * a.Lq * a.H * (a.d / 4);
-        const dim3 grid((uint32_t)((n + 255) / 256)), block(256);
+        const dim3 grid((uint32_t)((n + 63) / 64)), block(64);
         if (dt == DT_F32) PPIPE_LAUNCH(attention_join_kernel<float>, grid, block, 0, s, a, p);
         else if (dt == DT_F16) PPIPE_LAUNCH(attention_join_kernel<_Float16>, grid, block, 0, s, a, p);
         else PPIPE_LAUNCH(attention_join_kernel<__bf16>, grid, block, 0, s, a, p);

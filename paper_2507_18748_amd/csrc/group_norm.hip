@@ -405,12 +405,19 @@ group_norm_kernel(GroupNormArgs a, NormPlan p, float* part)
                 v[e] = norm_act<decltype(act)::value>(
                     __builtin_fmaf(ESZ == 2 ? v[e] : v[e] - mean[e % S], ga[e], be[e]));
             T* dst = (T*)((uint8_t*)y + off);
+            const uint4 w = pack<T, V>(v);
             if (!ends || (inside(i, 0) && inside(i, V - 1))) {
-                *(uint4*)dst = pack<T, V>(v);
+                *(uint4*)dst = w;
             } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (inside(i, e)) dst[e] = (T)v[e];
+                // element by element, not unrolled: the code would outgrow the rest
+#pragma unroll 1
+                for (int e = 0; e < V; ++e) {
+                    if (!inside(i, e)) continue;
+                    const int k = e * ESZ / 4;
+                    const uint32_t x = k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w;
+                    if constexpr (ESZ == 4) ((uint32_t*)dst)[e] = x;
+                    else ((uint16_t*)dst)[e] = (uint16_t)(x >> (16 * (e & 1)));
+                }
             }
         }
     });
@@ -515,7 +522,8 @@ void launch_norm(const GroupNormArgs& a, const NormPlan& p, float* part, hipStre
     if (!p.single && !p.whole) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, MIXED>), grid, dim3(NT), 0, s, a, p, part);
     else if (!p.single) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, SEVERAL>), grid, dim3(NT), 0, s, a, p, part);
     else if (p.whole && p.cv <= NT) PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ONE>), grid, dim3(NT), 0, s, a, p, part);
-    else PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ANY>), grid, dim3(NT), 0, s, a, p, part);
+    else if constexpr (R < NORM_R || sizeof(T) == 4)     // 16-bit: 65536 channels are 16 vectors a thread
+        PPIPE_LAUNCH((group_norm_kernel<T, NT, R, ANY>), grid, dim3(NT), 0, s, a, p, part);
 }
 
 template <typename T>
