@@ -256,8 +256,9 @@ int ppipe_partition_run(ppipe_partition* h, int32_t batch, const void* in,
 /* For callers that cannot allocate device memory (code under HIP graph
  * capture, allocation-free serving loops, harnesses that forbid hipMalloc):
  * ppipe_partition_run with the kernels' scratch memory -- split-K partial
- * sums, the fp32 logits of a final FC + softmax and the channel-padded input
- * of a stem -- taken from a fixed device array of PPIPE_STATIC_SCRATCH_BYTES
+ * sums, the fp32 logits of a final FC + softmax, the channel-padded input
+ * of a stem, statistics of group norms, rotated heads and parts of attention
+ * layers -- taken from a fixed device array of PPIPE_STATIC_SCRATCH_BYTES
  * that the library holds on every device it runs on (from the first create
  * on that device until the process ends), instead of the handle's
  * workspace.  Intermediate activations stay in the handle's buffers, which
@@ -389,13 +390,14 @@ int ppipe_attention_spans(int32_t* spans, int32_t batch, int32_t q_len, int32_t 
  *     s = softcap tanh(s / softcap)                       (softcap > 0)
  *     s = s - slopes[head] sum_a |q_position_ia - k_position_ja|   (slopes given)
  * Query head h reads key head h / (heads / kv_heads).  A query that sees no key
- * gets zeros, and so does one whose scores are all -inf.  Keys that a query does not see never change its
- * output, whatever they hold (NaN and infinities included). */
+ * gets zeros, and so does one whose scores are all -inf.  Keys that a query
+ * does not see never change its output, whatever they hold (NaN and infinities
+ * included). */
 typedef struct {
     int32_t dtype;
     int32_t batch, q_len, kv_len;
     int32_t heads, kv_heads, head_dim;        /* head_dim: a multiple of 8, at most 256 */
-    float scale, softcap;                     /* finite; softcap 0: none */
+    float scale, softcap;                     /* up to 2^100; softcap 0: none */
     int32_t axes;                             /* of the positions, 1 .. 3; 0 without slopes */
     int64_t q_strides[3], k_strides[3], v_strides[3], out_strides[3];
                                               /* between batch items, tokens, heads; below 2^22
@@ -410,8 +412,8 @@ int64_t ppipe_attention_workspace(const ppipe_attention_desc* desc);
 /* q, out: [batch][q_len][heads][head_dim], k, v: [batch][kv_len][kv_heads]
  * [head_dim] in dtype, by their strides (batch items of k and v may share
  * memory).  slopes: device fp32 [heads] with q_positions, k_positions: device
- * int32 [batch][q_len or kv_len][axes], or all three NULL.  spans: device int32
- * [batch][q_len][2], first and end of the keys that a query sees (cut to
+ * int32 [batch][q_len or kv_len][axes] (a sum of distances below 2^32), or all
+ * three NULL.  spans: device int32 [batch][q_len][2], first and end of the keys that a query sees (cut to
  * [0, kv_len]); NULL: all.  out must not overlap the inputs or itself.
  * workspace: ppipe_attention_workspace bytes.  Returns a status. */
 int ppipe_attention(const ppipe_attention_desc* desc, const void* q, const void* k, const void* v,

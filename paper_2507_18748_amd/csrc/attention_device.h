@@ -162,9 +162,14 @@ template <typename T> __device__ __forceinline__ float add2(uint32_t u, float c)
 
 // SPLITK: the waves of a block share one tile of rows and take key tiles in
 // turn, each with LDS of its own and no barrier (few rows, long caches: bound
-// by the bytes in flight).  Otherwise they take rows of their own and share
-// the key tiles.
-template <typename T, int DP, int QT, bool SPLITK> struct AttentionTile {
+// by memory; single tokens of 16 streams, 32 heads on 8 of 128, up to 16384 keys, f16:
+// 149 us, 5.0 TB/s).  Otherwise they take rows of their own and share
+// the key tiles (bound by the matrix cores and, heads of 64 and less or with cap or
+// bias, by the vector instructions of a score; 4 x 64x64 maps, 16 heads of 128, bf16:
+// 510-535 us, 1.03-1.08 PFLOP/s; 8 x 64x64 maps, 16 heads of 64, f16: 612 us, 0.9 PFLOP/s).
+// A key tile is 64 keys, two stages of it 64 KB at heads of 128, so two blocks fit
+// a CU; from heads of 136 on 32 keys, whose scores and weights leave the registers room.
+template <typename T, int DP, bool SPLITK> struct AttentionTile {
     static constexpr int ESZ = (int)sizeof(T);
     static constexpr int CH = DP * ESZ / 16;                    // 16-byte vectors of a row
     static constexpr int BK = SPLITK || DP * ESZ > 256 * (ESZ / 2) ? 32 : 64;
@@ -175,8 +180,8 @@ template <typename T, int DP, int QT, bool SPLITK> struct AttentionTile {
     static constexpr int STAGES = 2 * (SPLITK ? NW : 1);
     static constexpr int JOIN = SPLITK && NW > 1 ? NW * 32 * (DP + 2) * 4 : 0;
     static constexpr int LDS = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
-    static constexpr int WAVES = ESZ == 2 && DP <= 128 && QT == 1 && !SPLITK ? 2 : 1;   // per SIMD
-    static constexpr int ROWS = SPLITK ? 32 : 32 * QT * NW;     // rows of a block
+    static constexpr int WAVES = ESZ == 2 && DP <= 128 && !SPLITK ? 2 : 1;   // per SIMD
+    static constexpr int ROWS = SPLITK ? 32 : 32 * NW;     // rows of a block
     static constexpr int NI = BK * CH / 64;                     // wave loads of a K or V tile
     static constexpr int NL = SPLITK ? NI : NI / NW;            // of them, one wave's
     // LDS has 64 banks: 16 lanes of a 16-byte read, 32 of an 8-byte one must lie in
@@ -193,12 +198,12 @@ template <typename T, int DP, int QT, bool SPLITK> struct AttentionTile {
     }
 };
 
-template <typename T, int DP, int QT, bool SPLITK, bool EXTRA>
-__global__ void __launch_bounds__((AttentionTile<T, DP, QT, SPLITK>::NW * 64),
-                                  (AttentionTile<T, DP, QT, SPLITK>::WAVES))
+template <typename T, int DP, bool SPLITK, bool EXTRA>
+__global__ void __launch_bounds__((AttentionTile<T, DP, SPLITK>::NW * 64),
+                                  (AttentionTile<T, DP, SPLITK>::WAVES))
 attention_kernel(AttentionArgs a, AttentionPlan p)
 {
-    using TL = AttentionTile<T, DP, QT, SPLITK>;
+    using TL = AttentionTile<T, DP, SPLITK>;
     constexpr int ESZ = TL::ESZ, CH = TL::CH, BK = TL::BK, KT = TL::KT, NW = TL::NW, NL = TL::NL;
     constexpr int DT = DP / 32, RB = DP * ESZ, KB = BK * RB;
     constexpr int EPV = 16 / ESZ;
@@ -228,58 +233,43 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
     }
     const int n = group / a.Hk, hk = group - n * a.Hk, G = a.H / a.Hk;
 
-    // ---- this lane's rows: query, span, bias ----
-    const int row0 = tile * TL::ROWS + (SPLITK ? 0 : wave * 32 * QT);
-    uint4 q[QT][CH / 2];
-    int lo[QT], hi[QT];
-    float slope[QT];
-    uint32_t qp[QT][3];
-    int wlo = 0x7fffffff, whi = 0, wlo_max = 0, whi_min = 0x7fffffff;
+    // ---- this lane's row: query, span, bias ----
+    const int row0 = tile * TL::ROWS + (SPLITK ? 0 : wave * 32);
+    uint4 q[CH / 2];
+    const int r = row0 + col;
+    const bool ok = r < p.rows;
+    const int i = ok ? r / G : 0, h = hk * G + (ok ? r - i * G : 0);
+    const T* qr = (const T*)a.q + n * a.qs[0] + i * a.qs[1] + h * a.qs[2];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        const int r = row0 + 32 * t + col;
-        const bool ok = r < p.rows;
-        const int i = ok ? r / G : 0, h = hk * G + (ok ? r - i * G : 0);
-        const T* qr = (const T*)a.q + n * a.qs[0] + i * a.qs[1] + h * a.qs[2];
-#pragma unroll
-        for (int c = 0; c < CH / 2; ++c) {
-            const int e = (2 * c + half) * EPV;
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (ok && e < a.d && p.sign) u = *(const uint4*)(qr + e);
-            if (p.sign < 0) {
-                const uint32_t m = ESZ == 4 ? 0x80000000u : 0x80008000u;
-                u.x ^= m; u.y ^= m; u.z ^= m; u.w ^= m;
-            }
-            q[t][c] = u;
+    for (int c = 0; c < CH / 2; ++c) {
+        const int e = (2 * c + half) * EPV;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (ok && e < a.d && p.sign) u = *(const uint4*)(qr + e);
+        if (p.sign < 0) {
+            const uint32_t m = ESZ == 4 ? 0x80000000u : 0x80008000u;
+            u.x ^= m; u.y ^= m; u.z ^= m; u.w ^= m;
         }
-        lo[t] = 0;
-        hi[t] = ok ? a.Lk : 0;
-        if (ok && a.spans) {
-            const int* sp = a.spans + n * a.sps + 2 * (int64_t)i;
-            lo[t] = max(sp[0], 0);
-            hi[t] = min(sp[1], a.Lk);
-        }
-        if (hi[t] <= lo[t]) lo[t] = hi[t] = 0;
-        if (hi[t] > lo[t]) {
-            wlo = min(wlo, lo[t]);
-            whi = max(whi, hi[t]);
-        }
-        if (ok) {
-            wlo_max = max(wlo_max, lo[t]);
-            whi_min = min(whi_min, hi[t]);
-        }
-        if constexpr (EXTRA) {
-            slope[t] = a.slopes && ok ? a.slopes[h] * p.slope : 0.0f;
-#pragma unroll
-            for (int x = 0; x < 3; ++x)
-                qp[t][x] = a.slopes && ok && x < a.A
-                               ? (uint32_t)a.qpos[n * a.qps + (int64_t)i * a.A + x] ^ 0x80000000u : 0u;
-        }
+        q[c] = u;
     }
-    wlo = wave_min(wlo);
-    whi = wave_max(whi);
-    wlo_max = wave_max(wlo_max);
-    whi_min = wave_min(whi_min);
+    int lo = 0, hi = ok ? a.Lk : 0;
+    if (ok && a.spans) {
+        const int* sp = a.spans + n * a.sps + 2 * (int64_t)i;
+        lo = max(sp[0], 0);
+        hi = min(sp[1], a.Lk);
+    }
+    if (hi <= lo) lo = hi = 0;
+    float slope = 0.0f;
+    uint32_t qp[3];
+    if constexpr (EXTRA) {
+        slope = a.slopes && ok ? a.slopes[h] * p.slope : 0.0f;
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+            qp[x] = a.slopes && ok && x < a.A
+                        ? (uint32_t)a.qpos[n * a.qps + (int64_t)i * a.A + x] ^ 0x80000000u : 0u;
+    }
+    // the wave's rows see keys from wlo to whi, and all of them those from wlo_max to whi_min
+    const int wlo = wave_min(hi > lo ? lo : 0x7fffffff), whi = wave_max(hi);
+    const int wlo_max = wave_max(lo), whi_min = wave_min(ok ? hi : 0x7fffffff);
 
     // ---- the block's keys, and this split's part of them in whole tiles ----
     int kbeg = wlo, kend = whi;
@@ -347,26 +337,19 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             }
     };
 
-    // the queries (and their positions) are here before the loop: else every tile would wait for all
-    // loads under way, the next tile's among them, before its first product
+    // the queries (and their positions) are here before the loop: else every tile
+    // would wait for all loads under way, the next tile's among them, before its
+    // first product
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-#pragma unroll
-        for (int c = 0; c < CH / 2; ++c)
-            asm volatile("" : "+v"(q[t][c].x), "+v"(q[t][c].y), "+v"(q[t][c].z), "+v"(q[t][c].w));
-        if constexpr (EXTRA)
-            asm volatile("" : "+v"(slope[t]), "+v"(qp[t][0]), "+v"(qp[t][1]), "+v"(qp[t][2]));
-    }
+    for (int c = 0; c < CH / 2; ++c)
+        asm volatile("" : "+v"(q[c].x), "+v"(q[c].y), "+v"(q[c].z), "+v"(q[c].w));
+    if constexpr (EXTRA)
+        asm volatile("" : "+v"(slope), "+v"(qp[0]), "+v"(qp[1]), "+v"(qp[2]));
 
-    accx16 o[QT][DT];
-    float M[QT], l[QT];
+    accx16 o[DT];
+    float M = -INFINITY, l = 0.0f;       // running maximum (a power of two) and sum of weights
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-        M[t] = -INFINITY;
-        l[t] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[t][d] = accx16{};
-    }
+    for (int d = 0; d < DT; ++d) o[d] = accx16{};
     constexpr int KX = CH % 16 == 0 ? 8 : CH % 8 == 0 ? 4 : 2;    // vector pairs that the swizzle mixes
     const int kswz = TL::kswz(col);
     const uint32_t kread = (uint32_t)(col * RB + ((half ^ kswz) * 16));
@@ -394,22 +377,19 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
         asm volatile("" : "+v"(vat[0]), "+v"(vat[1]), "+v"(vat[2]), "+v"(vat[3]));
 
         // ---- scores ----
-        accx16 s[QT][KT];
+        accx16 s[KT];
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int c = 0; c < CH / 2; ++c) {
                 const uint4 kf = lds_read16(kat[c % KX] + (c / KX) * (32 * KX) + k * 32 * RB);
-#pragma unroll
-                for (int t = 0; t < QT; ++t) {
-                    if (c == 0) s[t][k] = accx16{};
-                    Mfma32<T>::step(kf, q[t][c], s[t][k]);
-                }
+                if (c == 0) s[k] = accx16{};
+                Mfma32<T>::step(kf, q[c], s[k]);
             }
         // six reads ahead of the products (two, the compiler's choice, leave each
         // product waiting for LDS)
         {
-            constexpr int N = KT * (CH / 2), PER = QT * (ESZ == 4 ? 4 : 1), AHEAD = N < 6 ? N : 6;
+            constexpr int N = KT * (CH / 2), PER = ESZ == 4 ? 4 : 1, AHEAD = N < 6 ? N : 6;
             __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
             for (int i = 0; i < N - AHEAD; ++i) {
@@ -422,24 +402,21 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             // one branch for the tile, not for each score
             auto each = [&](auto&& f) {
 #pragma unroll
-                for (int t = 0; t < QT; ++t)
+                for (int k = 0; k < KT; ++k)
 #pragma unroll
-                    for (int k = 0; k < KT; ++k)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[t][k][i] = f(s[t][k][i]);
+                    for (int i = 0; i < 16; ++i) s[k][i] = f(s[k][i]);
             };
             if (p.cap_mode == CAP_EXACT) {
                 if constexpr (ESZ == 4)
                     each([&](float v) { return a.cap * tanhf(v * p.pre / a.cap); });
                 else
                     each([&](float v) {
-                        const float x = v * (p.pre / a.cap), y = x * x;
+                        const float u = v * p.pre, x = v * (p.pre / a.cap), y = x * x;
                         const float e = __builtin_amdgcn_exp2f(v * p.capc);
-                        const float far = __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(e + 1.0f), 1.0f);
+                        const float far = __builtin_fmaf(-p.capk, __builtin_amdgcn_rcpf(e + 1.0f), a.cap);
                         float near = __builtin_fmaf(y, -0.053968254f, 0.13333333f);
                         near = __builtin_fmaf(y, near, -0.33333333f);
-                        near = __builtin_fmaf(x * y, near, x);
-                        return a.cap * (fabsf(x) < 0.125f ? near : far);
+                        return fabsf(x) < 0.125f ? __builtin_fmaf(u * y, near, u) : far;
                     });
             } else if (p.cap_mode == CAP_ALONE) {
                 each([&](float v) {
@@ -464,15 +441,13 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                         for (int x = 0; x < A; ++x)
                             kp[x] = lds_read16(src + 2 * KB + x * 256 + (32 * k + 8 * g + 4 * half) * 4);
 #pragma unroll
-                        for (int t = 0; t < QT; ++t)
+                        for (int b = 0; b < 4; ++b) {
+                            uint32_t dist = 0;
 #pragma unroll
-                            for (int b = 0; b < 4; ++b) {
-                                uint32_t dist = 0;
-#pragma unroll
-                                for (int x = 0; x < A; ++x)
-                                    dist = sad(qp[t][x], word(kp[x], b) ^ 0x80000000u, dist);
-                                s[t][k][4 * g + b] = __builtin_fmaf(-slope[t], (float)dist, s[t][k][4 * g + b]);
-                            }
+                            for (int x = 0; x < A; ++x)
+                                dist = sad(qp[x], word(kp[x], b) ^ 0x80000000u, dist);
+                            s[k][4 * g + b] = __builtin_fmaf(-slope, (float)dist, s[k][4 * g + b]);
+                        }
                     }
             };
             if (a.slopes) {
@@ -483,57 +458,52 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
         }
         if constexpr (!whole) {
 #pragma unroll
-            for (int t = 0; t < QT; ++t)
-#pragma unroll
-                for (int k = 0; k < KT; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int j = k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4;
-                        if (j < lo[t] || j >= hi[t]) s[t][k][i] = -INFINITY;
-                    }
-        }
-
-        // ---- running maximum and sum, weights ----
-        uint4 pf[QT][KT * 2];
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            float mx = s[t][0][0];
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][k][i]);
-            mx = half_max(mx) * p.c;
-            // the maximum follows only when weights would pass 2^8: they stay
-            // within the 16-bit range and the sums within fp32
-            if (__any(mx > M[t] + 8.0f)) {
-                const float mn = fmaxf(M[t], mx);
-                const float alpha = M[t] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[t] - mn);
-                M[t] = mn;
-                l[t] *= alpha;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
-            }
-            // weights of f16 are kept 2^6 up (at most 2^14), away from its small end
-            constexpr float UP = std::is_same<T, _Float16>::value ? 6.0f : 0.0f;
-            const float base = (M[t] == -INFINITY ? 0.0f : M[t]) - UP;
-#pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    s[t][k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k][i], p.c, -base));
-                    if constexpr (ESZ == 4) l[t] += s[t][k][i];
-                }
-            if constexpr (ESZ == 2)
-#pragma unroll
-                for (int k = 0; k < 2 * KT; ++k) {
-                    auto w = [&](int i) { return s[t][k / 2][8 * (k % 2) + i]; };
-                    // one rounding of the weights to the storage type: the matrix
-                    // instruction takes both operands in it
-                    pf[t][k] = make_uint4(pack2<T>(w(0), w(1)), pack2<T>(w(2), w(3)),
-                                          pack2<T>(w(4), w(5)), pack2<T>(w(6), w(7)));
-                    l[t] = add2<T>(pf[t][k].w, add2<T>(pf[t][k].z, add2<T>(pf[t][k].y, add2<T>(pf[t][k].x, l[t]))));
+                    const int j = k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4;
+                    if (j < lo || j >= hi) s[k][i] = -INFINITY;
                 }
         }
+
+        // ---- running maximum and sum, weights ----
+        uint4 pf[KT * 2];
+        float mx = s[0][0];
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[k][i]);
+        mx = half_max(mx) * p.c;
+        // the maximum follows only when weights would pass 2^8: they stay
+        // within the 16-bit range and the sums within fp32
+        if (__any(mx > M + 8.0f)) {
+            const float mn = fmaxf(M, mx);
+            const float alpha = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn);
+            M = mn;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= alpha;
+        }
+        // weights of f16 are kept 2^6 up (at most 2^14), away from its small end
+        constexpr float UP = std::is_same<T, _Float16>::value ? 6.0f : 0.0f;
+        const float base = (M == -INFINITY ? 0.0f : M) - UP;
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][i], p.c, -base));
+                if constexpr (ESZ == 4) l += s[k][i];
+            }
+        if constexpr (ESZ == 2)
+#pragma unroll
+            for (int k = 0; k < 2 * KT; ++k) {
+                auto w = [&](int i) { return s[k / 2][8 * (k % 2) + i]; };
+                // one rounding of the weights to the storage type: the matrix
+                // instruction takes both operands in it
+                pf[k] = make_uint4(pack2<T>(w(0), w(1)), pack2<T>(w(2), w(3)),
+                                   pack2<T>(w(4), w(5)), pack2<T>(w(6), w(7)));
+                l = add2<T>(pf[k].w, add2<T>(pf[k].z, add2<T>(pf[k].y, add2<T>(pf[k].x, l))));
+            }
 
         // ---- values ----
         // Keys that only some rows see may hold NaN or infinities, and 0 x NaN
@@ -567,9 +537,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                 }
                 if (whole || clean) {
 #pragma unroll
-                    for (int k = 0; k < 2 * KT; ++k)
-#pragma unroll
-                        for (int t = 0; t < QT; ++t) Mfma32<T>::step(f[k], pf[t][k], o[t][d]);
+                    for (int k = 0; k < 2 * KT; ++k) Mfma32<T>::step(f[k], pf[k], o[d]);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 2 * KT; ++k)
@@ -583,14 +551,11 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                             };
                             const int j = k0 + 16 * k + 4 * (e / 8) + (e & 3) + 8 * ((e >> 2) & 1);
                             const uint4 vk = only(f[k]);
+                            accx16 one = accx16{};
+                            Mfma32<T>::step(vk, only(pf[k]), one);
+                            const bool sees = j >= lo && j < hi;
 #pragma unroll
-                            for (int t = 0; t < QT; ++t) {
-                                accx16 one = accx16{};
-                                Mfma32<T>::step(vk, only(pf[t][k]), one);
-                                const bool sees = j >= lo[t] && j < hi[t];
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[t][d][i] += sees ? one[i] : 0.0f;
-                            }
+                            for (int i = 0; i < 16; ++i) o[d][i] += sees ? one[i] : 0.0f;
                         }
                 }
             }
@@ -614,10 +579,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                     if (whole || clean) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-#pragma unroll
-                            for (int t = 0; t < QT; ++t)
-                                o[t][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[i], s[t][k][i], o[t][d],
-                                                                               0, 0, 0);
+                            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[i], s[k][i], o[d], 0, 0, 0);
                     } else {
 #pragma unroll 1
                         for (int x = 0; x < 32; ++x) {
@@ -626,17 +588,14 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
                             float v = 0.0f;
 #pragma unroll
                             for (int y = 0; y < 16; ++y) v = y == i ? vf[y] : v;
+                            float w = 0.0f;
 #pragma unroll
-                            for (int t = 0; t < QT; ++t) {
-                                float w = 0.0f;
+                            for (int y = 0; y < 16; ++y) w = y == i ? s[k][y] : w;
+                            const bool sees = j >= lo && j < hi;
+                            const accx16 one = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                                half == e ? v : 0.0f, half == e ? w : 0.0f, accx16{}, 0, 0, 0);
 #pragma unroll
-                                for (int y = 0; y < 16; ++y) w = y == i ? s[t][k][y] : w;
-                                const bool sees = j >= lo[t] && j < hi[t];
-                                const accx16 one = __builtin_amdgcn_mfma_f32_32x32x2f32(
-                                    half == e ? v : 0.0f, half == e ? w : 0.0f, accx16{}, 0, 0, 0);
-#pragma unroll
-                                for (int y = 0; y < 16; ++y) o[t][d][y] += sees ? one[y] : 0.0f;
-                            }
+                            for (int y = 0; y < 16; ++y) o[d][y] += sees ? one[y] : 0.0f;
                         }
                     }
                 }
@@ -672,8 +631,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
         }
     }
 
-#pragma unroll
-    for (int t = 0; t < QT; ++t) l[t] += __shfl_xor(l[t], 32);
+    l += __shfl_xor(l, 32);
     auto row_of = [&](int r, int& i, int& h) {
         i = r / G;
         h = hk * G + r - i * G;
@@ -697,21 +655,18 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
         ml[1] = w;
     };
     if constexpr (!SPLITK || NW == 1) {
+        const int r = row0 + col;
+        if (r >= p.rows) return;
+        if (p.splits > 1 && half == 0) store_ml(r, M, l);
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            const int r = row0 + 32 * t + col;
-            if (r >= p.rows) continue;
-            if (p.splits > 1 && half == 0) store_ml(r, M[t], l[t]);
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int e = 32 * d + 8 * g + 4 * half;
-                    if (e < a.d)
-                        store4(r, e, l[t], o[t][d][4 * g], o[t][d][4 * g + 1], o[t][d][4 * g + 2],
-                               o[t][d][4 * g + 3]);
-                }
-        }
+            for (int g = 0; g < 4; ++g) {
+                const int e = 32 * d + 8 * g + 4 * half;
+                if (e < a.d)
+                    store4(r, e, l, o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2],
+                           o[d][4 * g + 3]);
+            }
     } else {
         // the waves' parts meet in LDS, each brought to the common maximum
         float* f = (float*)lds;
@@ -719,21 +674,21 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
         dma_wait<0>();
         __syncthreads();
         if (half == 0) {
-            ml[(wave * 32 + col) * 2] = M[0];
-            ml[(wave * 32 + col) * 2 + 1] = l[0];
+            ml[(wave * 32 + col) * 2] = M;
+            ml[(wave * 32 + col) * 2 + 1] = l;
         }
         __syncthreads();
         float m = -INFINITY;
 #pragma unroll
         for (int w = 0; w < NW; ++w) m = fmaxf(m, ml[(w * 32 + col) * 2]);
-        const float scale = M[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[0] - m);
+        const float scale = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - m);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *(float4*)&f[(wave * 32 + col) * DP + 32 * d + 8 * g + 4 * half] =
-                    make_float4(o[0][d][4 * g] * scale, o[0][d][4 * g + 1] * scale,
-                                o[0][d][4 * g + 2] * scale, o[0][d][4 * g + 3] * scale);
+                    make_float4(o[d][4 * g] * scale, o[d][4 * g + 1] * scale,
+                                o[d][4 * g + 2] * scale, o[d][4 * g + 3] * scale);
         __syncthreads();
         const int rows = min(32, p.rows - row0);
         for (int x = threadIdx.x; x < rows * (DP / 4); x += NW * 64) {
@@ -762,12 +717,12 @@ void launch_tile(const AttentionArgs& a, const AttentionPlan& p, const Attention
     const dim3 grid((uint32_t)c.blocks);
     const bool extra = a.cap > 0.0f || a.slopes;
     if (c.splitk) {
-        constexpr int NT = 64 * AttentionTile<T, DP, 1, true>::NW;
-        if (extra) PPIPE_LAUNCH((attention_kernel<T, DP, 1, true, true>), grid, dim3(NT), 0, s, a, p);
-        else PPIPE_LAUNCH((attention_kernel<T, DP, 1, true, false>), grid, dim3(NT), 0, s, a, p);
+        constexpr int NT = 64 * AttentionTile<T, DP, true>::NW;
+        if (extra) PPIPE_LAUNCH((attention_kernel<T, DP, true, true>), grid, dim3(NT), 0, s, a, p);
+        else PPIPE_LAUNCH((attention_kernel<T, DP, true, false>), grid, dim3(NT), 0, s, a, p);
     } else {
-        if (extra) PPIPE_LAUNCH((attention_kernel<T, DP, 1, false, true>), grid, dim3(256), 0, s, a, p);
-        else PPIPE_LAUNCH((attention_kernel<T, DP, 1, false, false>), grid, dim3(256), 0, s, a, p);
+        if (extra) PPIPE_LAUNCH((attention_kernel<T, DP, false, true>), grid, dim3(256), 0, s, a, p);
+        else PPIPE_LAUNCH((attention_kernel<T, DP, false, false>), grid, dim3(256), 0, s, a, p);
     }
 }
 

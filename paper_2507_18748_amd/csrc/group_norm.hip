@@ -13,6 +13,9 @@
 // it writes the outputs at once: one read, one write, one launch.  Larger maps
 // take two launches: slabs leave their mean and sum of squared differences,
 // the second launch joins those (Chan's formula) and reads the map again.
+//
+// 64 maps of 56x56x256 in 32 groups, bf16: 54 us, 3.8 TB/s (a copy of the bytes: 41); one
+// of 14x14x256: 4.6 us.
 #include "gemm_device.h"
 
 #include <algorithm>

@@ -167,8 +167,9 @@ int ppipe::check_attention(const ppipe_attention_desc& t, const std::string& who
     if (t.head_dim < 8 || t.head_dim > HEAD_DIM_MAX || t.head_dim % 8)
         return unsupported(who + "head_dim must be a multiple of 8, at most " +
                            std::to_string(HEAD_DIM_MAX));
-    if (!std::isfinite(t.scale) || !std::isfinite(t.softcap) || t.softcap < 0.0f)
-        return bad(who + "scale and softcap must be finite, softcap >= 0");
+    // (an infinity or a NaN fails these)
+    if (!(std::fabs(t.scale) <= 0x1p100f) || !(t.softcap >= 0.0f && t.softcap <= 0x1p100f))
+        return bad(who + "scale and softcap must be at most 2^100, softcap >= 0");
     if (t.axes < 0 || t.axes > 3) return bad(who + "positions have one to three axes");
     if (t.spans_stride % 2) return bad(who + "spans stride must be even");
     if (t.heads > MAX_HEADS || t.kv_len > ATTENTION_MAX_LEN || t.q_len > ATTENTION_MAX_LEN ||

@@ -85,7 +85,7 @@ def att(q=P, k=2 * P, v=3 * P, out=4 * P, dtype="f16", batch=2, lq=5, lk=7, head
     (dict(heads=3), -1), (dict(heads=0), -1), (dict(kv=0), -1), (dict(batch=-1), -1),
     (dict(lq=-1), -1), (dict(lk=-1), -1), (dict(scale=float("nan")), -1),
     (dict(scale=float("inf")), -1), (dict(cap=-1.0), -1), (dict(cap=float("nan")), -1),
-    (dict(axes=4), -1), (dict(axes=-1), -1), (dict(slopes=P), -1),
+    (dict(scale=2e30), -1), (dict(cap=2e30), -1), (dict(axes=4), -1), (dict(axes=-1), -1), (dict(slopes=P), -1),
     (dict(slopes=P, qp=P, kp=P, axes=0), -1), (dict(slopes=P, qp=P, axes=2), -1),
     (dict(qp=P, kp=P, axes=2), -1), (dict(q=0), -1), (dict(k=0), -1), (dict(v=0), -1),
     (dict(out=0), -1), (dict(q=P + 8), -1), (dict(out=P + 2), -1), (dict(spans=P + 4), -1),
