@@ -134,14 +134,6 @@ __device__ __forceinline__ uint32_t sad(uint32_t a, uint32_t b, uint32_t c)
     return d;
 }
 
-// Zero, or NaN if one of two 16-bit values is not finite.
-template <typename T> __device__ __forceinline__ float not_finite(uint32_t u)
-{
-    T e[2];
-    __builtin_memcpy(e, &u, 4);
-    return (float)e[0] * 0.0f + (float)e[1] * 0.0f;
-}
-
 // Two values rounded to a 16-bit type, and a + b + c of such a pair: the sum of
 // the weights as the products with the values see them.
 typedef float floatx2 __attribute__((ext_vector_type(2)));
@@ -158,6 +150,16 @@ template <typename T> __device__ __forceinline__ float add2(uint32_t u, float c)
                                                (pair){(T)1.0f, (T)1.0f}, c, false);
     else
         return __builtin_amdgcn_fdot2(__builtin_bit_cast(pair, u), (pair){(T)1.0f, (T)1.0f}, c, false);
+}
+
+// z, or NaN if one of two 16-bit values is not finite.
+template <typename T> __device__ __forceinline__ float add_not_finite(uint32_t u, float z)
+{
+    typedef T pair __attribute__((ext_vector_type(2)));
+    if constexpr (std::is_same<T, __bf16>::value)
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, u), (pair){}, z, false);
+    else
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(pair, u), (pair){}, z, false);
 }
 
 // SPLITK: the waves of a block share one tile of rows and take key tiles in
@@ -457,13 +459,18 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
             }
         }
         if constexpr (!whole) {
+            // a bit for each of 32 keys, spread to a word that takes the score or -inf
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
+            for (int k = 0; k < KT; ++k) {
+                const int from = min(max(lo - k0 - 32 * k, 0), 32), to = min(max(hi - k0 - 32 * k, 0), 32);
+                const uint32_t seen = (uint32_t)((1ull << to) - 1) & ~(uint32_t)((1ull << from) - 1);
+                const uint32_t mine = seen >> (4 * half);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int j = k0 + 32 * k + 8 * (i / 4) + 4 * half + i % 4;
-                    if (j < lo || j >= hi) s[k][i] = -INFINITY;
+                    const uint32_t take = (uint32_t)((int)(mine << (31 - 8 * (i / 4) - i % 4)) >> 31);
+                    s[k][i] = __uint_as_float((__float_as_uint(s[k][i]) & take) | (0xff800000u & ~take));
                 }
+            }
         }
 
         // ---- running maximum and sum, weights ----
@@ -532,7 +539,7 @@ attention_kernel(AttentionArgs a, AttentionPlan p)
 #pragma unroll
                     for (int k = 0; k < 2 * KT; ++k)
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) z += not_finite<T>(word(f[k], w));
+                        for (int w = 0; w < 4; ++w) z = add_not_finite<T>(word(f[k], w), z);
                     clean = !__any(!(z == 0.0f));
                 }
                 if (whole || clean) {
