@@ -92,9 +92,11 @@ __global__ void __launch_bounds__(64) attention_join_kernel(AttentionArgs a, Att
 // 18.6 / 15.8, f32 of 64 x 1 76 / 36; beyond one round: 32x32 of 128 x 3 27.6 / 45.6,
 // 14x14 of 32 x 16 8.0 / 11.6.
 // Few blocks: the keys are split further among blocks until the chip is filled;
-// each part keeps at least 512 keys for what the join costs (fp32, whose tiles
-// take several times as long: 256 of heads of 64, 64 of 256; 32 and 512 keys
-// there: 500 tokens of 8 heads of 128 32.7 / 44.6 / 45.1 us).
+// each part keeps at least 512 keys of heads of 64, 256 from 128 on, for what the
+// join costs (256 and 512: 900 tokens of 2 heads of 64 12.3 / 11.0 us, a token of 8
+// heads of 128 against 4000 keys 15.2 / 18.6; fp32, whose tiles take several times
+// as long: 256 of heads of 64, 64 of 256; 32 and 512 keys there: 500 tokens of 8
+// heads of 128 32.7 / 44.6 / 45.1 us).
 AttentionChoice choose(int dt, const AttentionArgs& a, int cus)
 {
     AttentionChoice c;
@@ -104,7 +106,8 @@ AttentionChoice choose(int dt, const AttentionArgs& a, int cus)
     const int per = c.splitk ? 32 : 128;
     c.tiles = (int)((rows + per - 1) / per);
     c.splits = 1;
-    const int part = dt == DT_F32 ? std::max(64, 256 * 64 / a.d) : 512;
+    const int part = dt == DT_F32 ? std::max(64, 256 * 64 / a.d)
+                                  : std::min(512, std::max(256, 512 * 64 / a.d));
     while (c.splitk && c.splits < 64 && groups * c.tiles * c.splits < 2 * cus &&
            a.Lk / (c.splits * 2) >= part)
         c.splits *= 2;
