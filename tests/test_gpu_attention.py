@@ -328,6 +328,60 @@ def test_rest_of_a_cache_is_not_read(dtype, d, lk, lo, hi):
     R.check(call(q, k, v, torch.empty_like(q), dtype, d ** -0.5, span=span), ref, bound, dtype)
 
 
+# Grids beyond one round of 32-row blocks: the waves of a block share key tiles.
+# 2100 queries of 8 key heads (a multiple of the XCDs) or 9 of them (not one).
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [24, 64, 80, 128, 160, 256])
+@pytest.mark.parametrize("mask", ["none", "documents", "prefix", "any"])
+def test_many_rows(dtype, d, mask):
+    lq, lk, hk = 2100, 2100 if mask in ("documents", "prefix") else 333, 8 if d in (64, 128) else 9
+    kw = dict(n=1, lq=lq, lk=lk)
+    span = None
+    if mask == "documents":
+        span = make_spans(offsets=[[0, 7, 7, 300, 1111, 1500, 2090]], **kw)
+    elif mask == "prefix":
+        span = make_spans(causal=True, offsets=[[0, 900, 2100]], prefix=[[130, 500]], **kw)
+    elif mask == "any":
+        g = torch.Generator().manual_seed(11)
+        span = torch.randint(-20, 360, (1, lq, 2), generator=g, dtype=torch.int32).cuda()
+    case(dtype, 1, lq, lk, hk, hk, d, span)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [32, 72, 128, 200])
+@pytest.mark.parametrize("axes,cap", [(0, 6.0), (1, 0.0), (2, 6.0), (3, 0.0), (2, 5000.0)])
+def test_many_rows_with_bias_and_cap(dtype, d, axes, cap):
+    lq, lk, h, hk = 1100, 190, 16, 8
+    slopes, qpos, kpos = bias(h, lq, lk, axes) if axes else (None, None, None)
+    g = torch.Generator().manual_seed(13)
+    span = torch.stack([torch.zeros(1, lq), torch.randint(0, lk + 1, (1, lq), generator=g)], -1)
+    for sp in (None, span.to(torch.int32).cuda().contiguous()):
+        case(dtype, 1, lq, lk, h, hk, d, sp, cap, slopes, qpos, kpos, size=3.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 136])
+def test_many_rows_do_not_see_hidden_values(dtype, d):
+    lq, lk, hk = 2200, 300, 8
+    q, k, v = tensors(dtype, 1, lq, lk, hk, hk, d, seed=21)
+    k, v = k.contiguous(), v.contiguous()
+    g = torch.Generator().manual_seed(22)
+    lo = torch.randint(0, lk, (1, lq), generator=g)
+    span = torch.stack([lo, lo + torch.randint(0, 90, (1, lq), generator=g)], -1)
+    span = span.to(torch.int32).cuda().contiguous()
+    bad = [3, 64, 130, 299]
+    k[:, bad[1]], v[:, bad[0]], v[:, bad[2], :, 5], v[:, bad[3]] = (float(x) for x in ("nan", "nan", "inf", "-inf"))
+    out = call(q, k, v, torch.empty(1, lq, hk, d, dtype=q.dtype, device="cuda"), dtype, d ** -0.5, span=span)
+    j = torch.tensor(bad, device="cuda")
+    hit = ((j >= span[0, :, :1]) & (j < span[0, :, 1:])).any(-1)
+    clean = ~hit
+    k2, v2 = k.clone(), v.clone()
+    k2[:, bad], v2[:, bad] = 0.0, 0.0
+    ref, bound = R.attention(q, k2, v2, d ** -0.5, span=span, dtype=dtype)
+    R.check(out[:, clean], ref[:, clean], bound[:, clean], dtype)
+    assert int(clean.sum()) > 100 and int(hit.sum()) > 100
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_infinite_scores(dtype):
     """All scores -inf: zeros; one +inf: NaN; some -inf: as if hidden."""
